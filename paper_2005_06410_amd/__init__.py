@@ -42,6 +42,10 @@ __all__ = [
     "release_workspace",
     "conv_out_size",
     "convgemm",
+    "linear",
+    "linear_backward",
+    "grad_norm",
+    "clip_grad_norm",
     "LtltError",
     "F64",
     "F32",
@@ -86,6 +90,22 @@ _SYMBOLS = {
     "convgemm_choice": ([ctypes.c_int] * 9 + [ctypes.c_void_p], ctypes.c_int),
     "convgemm_f32": ([ctypes.c_int] * 9 + [ctypes.c_void_p] * 3 + [ctypes.c_int] * 4 + [ctypes.c_void_p],
                      ctypes.c_int),
+    # include/linear.h
+    "convgemm_linear_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int], ctypes.c_int64),
+    "convgemm_linear": ([ctypes.c_int] + [ctypes.c_int64] * 3
+                        + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                           ctypes.c_void_p, ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int64] * 4
+                        + [ctypes.c_void_p], ctypes.c_int),
+    "convgemm_linear_backward_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 2, ctypes.c_int64),
+    "convgemm_linear_backward": ([ctypes.c_int] + [ctypes.c_int64] * 3
+                                 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64]
+                                 + [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_int]
+                                 + [ctypes.c_void_p, ctypes.c_int64] * 2
+                                 + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    "convgemm_grad_workspace": ([ctypes.c_int], ctypes.c_int64),
+    "convgemm_grad_norm": ([ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    "convgemm_grad_clip": ([ctypes.c_int] + [ctypes.c_void_p] * 4 + [ctypes.c_double] + [ctypes.c_void_p] * 2
+                           + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
 }
 
 
@@ -422,6 +442,246 @@ def convgemm(F, I, stride: int = 1, pad: int = 0, out=None, accumulate: bool = F
                                _stream_ptr(I.device))
     _check("convgemm_f32", code)
     return out
+
+
+# Layer operators (include/linear.h).
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_layer_codes = None
+
+
+def _layer_dtype(t) -> int:
+    global _layer_codes
+    if _layer_codes is None:
+        torch = _torch()
+        _layer_codes = {torch.float32: 1, torch.bfloat16: 4, torch.float16: 5}
+    code = _layer_codes.get(t.dtype)
+    if code is None:
+        raise TypeError("only float32, bfloat16 and float16 are supported")
+    return code
+
+
+def _activation(name) -> int:
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+    return code
+
+
+def _columns(t, rows: int, cols: int, name: str, like) -> int:
+    """The leading dimension of a (rows, cols) tensor stored with its first
+    index fastest, of `like`'s dtype and device."""
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must have shape {(rows, cols)}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must have X's dtype")
+    if t.device != like.device:
+        raise ValueError("all tensor arguments must be on the same GPU")
+    s0, s1 = t.stride()
+    if (rows > 1 and s0 != 1) or (cols > 1 and s1 < max(rows, 1)):
+        raise ValueError(f"{name} must be stored leftmost index fastest: stride(0) == 1, stride(1) >= {rows}")
+    return s1 if cols > 1 else max(rows, 1)
+
+
+def _weights(F, like):
+    """(kn, ci, order, leading dimension) of weights with either index fastest."""
+    if F.dim() != 2:
+        raise ValueError("F must be (kn, ci)")
+    if F.dtype != like.dtype:
+        raise TypeError("F must have X's dtype")
+    if F.device != like.device:
+        raise ValueError("all tensor arguments must be on the same GPU")
+    kn, ci = F.shape
+    s0, s1 = F.stride()
+    if (ci <= 1 or s1 == 1) and (kn <= 1 or s0 >= max(ci, 1)):
+        return kn, ci, 1, s0 if kn > 1 else max(ci, 1)
+    if (kn <= 1 or s0 == 1) and (ci <= 1 or s1 >= max(kn, 1)):
+        return kn, ci, 0, s1 if ci > 1 else max(kn, 1)
+    raise ValueError("F must have one index with stride 1 and no overlap along the other")
+
+
+def _on_device(t):
+    """Makes t's GPU the current one for a call."""
+    import contextlib
+    torch = _torch()
+    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _new_columns(rows: int, cols: int, like):
+    return _torch().empty((cols, rows), dtype=like.dtype, device=like.device).t()
+
+
+def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, keep_pre: bool = False):
+    """O = act(F X + bias) + residual, one matrix product with the rest in its
+    epilogue (``convgemm_linear``).
+
+    F: (kn, ci), either index fastest (the convolution's filters, or a row-major
+    weight as it is); X: (ci, t) and ``residual`` (kn, t) stored with the
+    leftmost index fastest (the transposed view of row-major activations);
+    ``bias``: (kn,).  All float32, bfloat16 or float16; sums and epilogue are
+    fp32, and each result is rounded once.  ``activation``: none, relu, gelu,
+    gelu_tanh or silu.
+
+    Returns O (kn, t) in the same storage (``out`` if given; it may be
+    ``residual`` itself), or (O, Z) with the pre-activation
+    Z = F X + bias for ``linear_backward`` where ``keep_pre`` is set."""
+    _require_gpu(X)
+    if X.dim() != 2:
+        raise ValueError("X must be (ci, t)")
+    code, act = _layer_dtype(X), _activation(activation)
+    kn, ci, order, ldf = _weights(F, X)
+    t = X.shape[1]
+    ldx = _columns(X, ci, t, "X", X)
+    bp = 0
+    if bias is not None:
+        if bias.shape != (kn,) or (kn > 1 and bias.stride(0) != 1):
+            raise ValueError(f"bias must be a contiguous tensor of {kn} values")
+        if bias.dtype != X.dtype:
+            raise TypeError("bias must have X's dtype")
+        _same_device(X, bias)
+        bp = bias.data_ptr()
+    rp, ldr = (0, 1) if residual is None else (residual.data_ptr(), _columns(residual, kn, t, "residual", X))
+    if out is None:
+        out = _new_columns(kn, t, X)
+    ldo = _columns(out, kn, t, "out", X)
+    Z = _new_columns(kn, t, X) if keep_pre else None
+    lib = load()
+    with _on_device(X):
+        need = lib.convgemm_linear_workspace(code, kn, ci, t, order)
+        ws = _workspace(need, X.device)
+        err = lib.convgemm_linear(code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, bp, act, rp, ldr,
+                                  Z.data_ptr() if keep_pre else 0, max(kn, 1), out.data_ptr(), ldo,
+                                  0 if ws is None else ws.data_ptr(), need, _stream_ptr(X.device))
+    _check("convgemm_linear", err)
+    return (out, Z) if keep_pre else out
+
+
+def _workspace(need: int, device):
+    """Scratch of a call, from torch's allocator: stream-ordered like the call."""
+    if need < 0:
+        raise ValueError(f"sizes out of range (argument {-need} of the layer)")
+    return _torch().empty(need, dtype=_torch().uint8, device=device) if need else None
+
+
+def linear_backward(F, X, dO, pre=None, activation: str = "none", needs=(True, True, True)):
+    """(dX, dF, dbias) of ``linear`` from dO = dL/dO (kn, t), stored like O
+    (``convgemm_linear_backward``); the residual's gradient is dO itself.
+
+    ``pre`` is the Z that ``linear(..., keep_pre=True)`` returned; without an
+    activation it is not needed.  dX is stored like X, dF in F's order.
+    ``needs`` leaves out what is not wanted (None is returned in its place)."""
+    _require_gpu(X)
+    if X.dim() != 2:
+        raise ValueError("X must be (ci, t)")
+    code, act = _layer_dtype(X), _activation(activation)
+    kn, ci, order, ldf = _weights(F, X)
+    t = X.shape[1]
+    ldx = _columns(X, ci, t, "X", X)
+    lddo = _columns(dO, kn, t, "dO", X)
+    zp, ldz = 0, 1
+    if act:
+        if pre is None:
+            raise ValueError("an activation's gradient needs the pre-activation (pre)")
+        zp, ldz = pre.data_ptr(), _columns(pre, kn, t, "pre", X)
+    torch = _torch()
+    dX = _new_columns(ci, t, X) if needs[0] else None
+    dF = (torch.empty((kn, ci), dtype=X.dtype, device=X.device) if order else _new_columns(kn, ci, X)) if needs[1] else None
+    dbias = torch.empty(kn, dtype=X.dtype, device=X.device) if needs[2] else None
+    lib = load()
+
+    def ptr(v):
+        return 0 if v is None else v.data_ptr()
+
+    with _on_device(X):
+        need = lib.convgemm_linear_backward_workspace(code, kn, ci, t, order, act)
+        ws = _workspace(need, X.device)
+        err = lib.convgemm_linear_backward(code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, dO.data_ptr(),
+                                           lddo, zp, ldz, act, ptr(dX), max(ci, 1), ptr(dF),
+                                           max(ci if order else kn, 1), ptr(dbias), ptr(ws), need,
+                                           _stream_ptr(X.device))
+    _check("convgemm_linear_backward", err)
+    return dX, dF, dbias
+
+
+def _dense(t) -> bool:
+    """Whether t's values fill its memory without gaps or overlap, in any order."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+def _grad_list(grads, what):
+    import array
+    grads = list(grads)
+    dev = None
+    ptrs, sizes, codes = array.array("Q"), array.array("q"), array.array("i")
+    for g in grads:
+        if dev is None:
+            _require_gpu(g)
+            dev = g.device
+        elif g.device != dev:
+            raise ValueError(f"all {what} must be on the same GPU")
+        if not _dense(g):
+            raise ValueError(f"{what} must be stored without gaps or overlap")
+        ptrs.append(g.data_ptr())
+        sizes.append(g.numel())
+        codes.append(_layer_dtype(g))
+    return grads, dev, ptrs, sizes, codes
+
+
+def grad_norm(grads):
+    """The 2-norm of all tensors of ``grads`` together, one float32 value on
+    their GPU (``convgemm_grad_norm``); squares are summed in fp64.
+
+    Tensors are float32, bfloat16 or float16 (mixed as they come), of any shape,
+    stored without gaps in any order.  An empty list is refused: it names no GPU."""
+    return _norm_and_clip(grads, None, None)
+
+
+def clip_grad_norm(grads, max_norm: float, out=None):
+    """Scales ``grads`` by c = min(1, max_norm / norm) with their joint norm
+    (``convgemm_grad_clip``), in place or into the tensors ``out`` (the same
+    shapes, types and strides).  Returns the norm before scaling, as
+    ``grad_norm`` does; nothing is copied to the host.
+
+    An infinite norm makes c zero and a NaN norm makes it NaN."""
+    if not max_norm >= 0:
+        raise ValueError("max_norm must be at least 0")
+    return _norm_and_clip(grads, float(max_norm), out)
+
+
+def _norm_and_clip(grads, max_norm, out):
+    grads, dev, ptrs, sizes, codes = _grad_list(grads, "gradients")
+    if not grads:
+        raise ValueError("no gradients")
+    optrs = ptrs
+    if out is not None:
+        outs, odev, optrs, osizes, ocodes = _grad_list(out, "outputs")
+        if odev != dev or osizes != sizes or ocodes != codes or any(
+                o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))
+                for o, g in zip(outs, grads)):
+            raise ValueError("out must have the gradients' shapes, types, strides and GPU")
+    torch = _torch()
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    lib = load()
+    count = len(grads)
+    need = lib.convgemm_grad_workspace(count)
+    ws = _workspace(need, dev)
+    a = [v.buffer_info()[0] for v in (ptrs, optrs, sizes, codes)]
+    with _on_device(norm):
+        s = _stream_ptr(dev)
+        if max_norm is None:
+            fn = "convgemm_grad_norm"
+            err = lib.convgemm_grad_norm(count, a[0], a[2], a[3], norm.data_ptr(), ws.data_ptr(), need, s)
+        else:
+            fn = "convgemm_grad_clip"
+            err = lib.convgemm_grad_clip(count, a[0], a[1], a[2], a[3], max_norm, norm.data_ptr(), ws.data_ptr(), need, s)
+    _check(fn, err)
+    return norm
 
 
 def device_status(device=None):

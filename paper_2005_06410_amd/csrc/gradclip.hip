@@ -1,0 +1,263 @@
+// The norm of many gradients together, and the gradients scaled to at most a
+// given norm, on gfx950: one pass that sums the squares and one that scales.
+//
+// Squares are formed and summed in fp64: a gradient of 1e30 or 1e-30 squares
+// without leaving the range, and the sum over 10^9 values keeps more digits
+// than its fp32 result shows.  Every workgroup takes a contiguous run of chunks
+// of the tensors laid end to end and writes one partial sum; the scaling pass
+// adds the partial sums in order in each of its workgroups, so the result does
+// not depend on which workgroup ends first and no third launch is needed.
+//
+// Bound by memory: 16-byte loads at any alignment, four in flight per thread.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "linear_common.h"
+
+namespace linear {
+namespace {
+
+constexpr int kList = 120;          // tensors of one launch: the list travels in the kernel's arguments
+constexpr int64_t kTensorLimit = 1ll << 37;   // values of one tensor: the chunks of a list are below 2^31
+constexpr int kParts = 2048;        // partial sums (workgroups of the first pass)
+constexpr int kChunkBytes = 32768;  // of one step of a workgroup
+
+struct List {
+  const void* g[kList];
+  void* out[kList];
+  int64_t n[kList];
+  int first[kList + 1];             // chunks before each tensor
+  unsigned char dtype[kList];
+  int count;
+};
+static_assert(sizeof(List) < 4000, "the list fits the kernel's arguments");
+
+__device__ inline double block_sum(double v) {
+  __shared__ double sh[4];
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = (sh[0] + sh[1]) + (sh[2] + sh[3]);
+  __syncthreads();
+  return v;
+}
+
+// The tensor that holds chunk c.
+__device__ inline int tensor_of(const List& l, int c) {
+  int lo = 0, hi = l.count;          // first[lo] <= c < first[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (l.first[mid] <= c) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+template <class T> __device__ inline double squares(const T* g, int64_t n) {
+  constexpr int V = kVec<T>;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  const int64_t whole = n / V;
+  int64_t i = threadIdx.x;
+  for (; i + 768 < whole; i += 1024) {
+    float v[4][V];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load_vec(g + (i + 256 * u) * V, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[u] = fma((double)v[u][j], (double)v[u][j], s[u]);
+  }
+  for (; i < whole; i += 256) {
+    float v[V];
+    load_vec(g + i * V, v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j & 3] = fma((double)v[j], (double)v[j], s[j & 3]);
+  }
+  if (threadIdx.x < n - whole * V) {
+    const double x = (double)(float)g[whole * V + threadIdx.x];
+    s[0] = fma(x, x, s[0]);
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+template <class T> __device__ inline void scale(const T* g, T* out, int64_t n, float c) {
+  constexpr int V = kVec<T>;
+  const int64_t whole = n / V;
+  int64_t i = threadIdx.x;
+  for (; i + 768 < whole; i += 1024) {
+    float v[4][V];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load_vec(g + (i + 256 * u) * V, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[u][j] *= c;
+      store_vec(out + (i + 256 * u) * V, v[u]);
+    }
+  }
+  for (; i < whole; i += 256) {
+    float v[V];
+    load_vec(g + i * V, v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] *= c;
+    store_vec(out + i * V, v);
+  }
+  if (threadIdx.x < n - whole * V) {
+    const int64_t j = whole * V + threadIdx.x;
+    out[j] = (T)((float)g[j] * c);
+  }
+}
+
+// Calls f(tensor, first value, values) for the chunks lo .. hi-1.
+template <class F> __device__ inline void for_chunks(const List& l, int lo, int hi, F f) {
+  if (lo >= hi) return;
+  for (int i = tensor_of(l, lo); lo < hi; ++i) {
+    const int end = min(hi, l.first[i + 1]);
+    if (end <= lo) continue;
+    const int64_t per = kChunkBytes / (l.dtype[i] == LINEAR_F32 ? 4 : 2);
+    const int64_t at = (int64_t)(lo - l.first[i]) * per;
+    f(i, at, min(l.n[i] - at, (int64_t)(end - lo) * per));
+    lo = end;
+  }
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(List l, double* part) {
+  const int chunks = l.first[l.count];
+  const int lo = (int)((int64_t)chunks * blockIdx.x / gridDim.x), hi = (int)((int64_t)chunks * (blockIdx.x + 1) / gridDim.x);
+  double s = 0.0;
+  for_chunks(l, lo, hi, [&](int i, int64_t at, int64_t n) {
+    if (l.dtype[i] == LINEAR_F32)
+      s += squares(static_cast<const float*>(l.g[i]) + at, n);
+    else if (l.dtype[i] == LINEAR_BF16)
+      s += squares(static_cast<const bf16*>(l.g[i]) + at, n);
+    else
+      s += squares(static_cast<const f16*>(l.g[i]) + at, n);
+  });
+  s = block_sum(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+// sqrt of the partial sums' total, the same in every workgroup.
+__device__ inline double total_norm(const double* part, int parts) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += 256) s += part[i];
+  return sqrt(block_sum(s));
+}
+
+__global__ __launch_bounds__(256) void total_kernel(const double* part, int parts, float* norm) {
+  const double v = total_norm(part, parts);
+  if (threadIdx.x == 0) *norm = (float)v;
+}
+
+__global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, int parts, double max_norm, float* norm) {
+  const double v = total_norm(part, parts);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  // a NaN norm gives a NaN factor
+  const float c = v <= max_norm ? 1.0f : (float)(max_norm / v);
+  const int chunks = l.first[l.count];
+  const int lo = (int)((int64_t)chunks * blockIdx.x / gridDim.x), hi = (int)((int64_t)chunks * (blockIdx.x + 1) / gridDim.x);
+  for_chunks(l, lo, hi, [&](int i, int64_t at, int64_t n) {
+    if (c == 1.0f && l.out[i] == l.g[i]) return;
+    if (l.dtype[i] == LINEAR_F32)
+      scale(static_cast<const float*>(l.g[i]) + at, static_cast<float*>(l.out[i]) + at, n, c);
+    else if (l.dtype[i] == LINEAR_BF16)
+      scale(static_cast<const bf16*>(l.g[i]) + at, static_cast<bf16*>(l.out[i]) + at, n, c);
+    else
+      scale(static_cast<const f16*>(l.g[i]) + at, static_cast<f16*>(l.out[i]) + at, n, c);
+  });
+}
+
+// Fills `l` with tensors from `from` on; returns the next one that did not fit.
+int take(List& l, int from, int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype) {
+  l.count = 0;
+  l.first[0] = 0;
+  for (; from < count && l.count < kList; ++from) {
+    if (n[from] == 0) continue;
+    const int64_t chunks = (n[from] * type_size(dtype[from]) + kChunkBytes - 1) / kChunkBytes;
+    const int i = l.count++;
+    l.g[i] = g[from];
+    l.out[i] = out ? out[from] : nullptr;
+    l.n[i] = n[from];
+    l.dtype[i] = (unsigned char)dtype[from];
+    l.first[i + 1] = l.first[i] + (int)chunks;
+  }
+  return from;
+}
+
+unsigned workgroups(const List& l) { return (unsigned)std::min(l.first[l.count], kParts); }
+
+int launches_of(int count) { return std::max(1, (count + kList - 1) / kList); }
+
+int run(int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype, double max_norm, float* norm,
+        void* workspace, hipStream_t s) {
+  double* part = static_cast<double*>(workspace);
+  int parts = 0;
+  List l;
+  for (int at = 0; at < count;) {
+    at = take(l, at, count, g, out, n, dtype);
+    if (l.count == 0) break;
+    norm_kernel<<<dim3(workgroups(l)), 256, 0, s>>>(l, part + parts);
+    parts += (int)workgroups(l);
+  }
+  hipError_t e = hipGetLastError();
+  bool told = false;
+  for (int at = 0; e == hipSuccess && out && at < count;) {
+    at = take(l, at, count, g, out, n, dtype);
+    if (l.count == 0) break;
+    scale_kernel<<<dim3(workgroups(l)), 256, 0, s>>>(l, part, parts, max_norm, told ? nullptr : norm);
+    told = true;
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && !told) {
+    total_kernel<<<1, 256, 0, s>>>(part, parts, norm);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
+}
+
+// Arguments shared by the two calls, by the norm call's numbering.
+int check(int count, const void* const* g, const int64_t* n, const int* dtype) {
+  if (count < 0) return 1;
+  if (count == 0) return 0;
+  if (!g) return 2;
+  if (!n) return 3;
+  if (!dtype) return 4;
+  for (int i = 0; i < count; ++i) {
+    if (n[i] < 0 || n[i] >= kTensorLimit) return 3;
+    if (!is_type(dtype[i])) return 4;
+    if (n[i] > 0 && !g[i]) return 2;
+  }
+  return 0;
+}
+
+}  // namespace
+}  // namespace linear
+
+extern "C" int64_t convgemm_grad_workspace(int count) {
+  if (count < 0) return -1;
+  return (int64_t)linear::launches_of(count) * linear::kParts * 8;
+}
+
+extern "C" int convgemm_grad_norm(int count, const void* const* g, const int64_t* n, const int* dtype, float* norm,
+                                  void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  if (int e = linear::check(count, g, n, dtype)) return -e;
+  if (!norm) return -5;
+  if (!workspace || ((uintptr_t)workspace & 15)) return -6;
+  if (workspace_bytes < convgemm_grad_workspace(count)) return -7;
+  return linear::run(count, g, nullptr, n, dtype, 0.0, norm, workspace, stream);
+}
+
+extern "C" int convgemm_grad_clip(int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype,
+                                  double max_norm, float* norm, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  if (int e = linear::check(count, g, n, dtype)) return e > 2 ? -(e + 1) : -e;
+  if (count > 0 && !out) return -3;
+  for (int i = 0; i < count; ++i)
+    if (n[i] > 0 && !out[i]) return -3;
+  if (!(max_norm >= 0.0)) return -6;
+  if (!norm) return -7;
+  if (!workspace || ((uintptr_t)workspace & 15)) return -8;
+  if (workspace_bytes < convgemm_grad_workspace(count)) return -9;
+  return linear::run(count, g, out, n, dtype, max_norm, norm, workspace, stream);
+}

@@ -1,0 +1,162 @@
+// Shared by the layer operators (linear.hip, linear_grad.hip): element types,
+// 16-byte vectors at any address, activations and the product's description.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "linear.h"
+
+namespace linear {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// Values of one 16-byte chunk.
+template <class T> constexpr int kVec = 16 / (int)sizeof(T);
+
+// kVec consecutive values as fp32, from and to any address the type allows: the
+// 16-byte accesses carry no alignment promise, which global memory serves in
+// hardware.
+template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Packed {
+  T v[kVec<T>];
+};
+
+template <class T> __device__ inline void load_vec(const T* p, float* out) {
+  const Packed<T> q = *reinterpret_cast<const Packed<T>*>(p);
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i) out[i] = (float)q.v[i];
+}
+
+template <class T> __device__ inline void store_vec(T* p, const float* v) {
+  Packed<T> q;
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i) q.v[i] = (T)v[i];
+  *reinterpret_cast<Packed<T>*>(p) = q;
+}
+
+constexpr float kTanhScale = 0.7978845608028654f;   // sqrt(2 / pi)
+constexpr float kTanhCubic = 0.044715f;
+
+// act(z) in fp32.  gelu takes Phi from erfc, which keeps its relative accuracy
+// for negative z; gelu_tanh takes (1 + tanh u) / 2 as the logistic function of
+// 2u, for the same reason.
+__device__ inline float act_value(float z, int act) {
+  switch (act) {
+    case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : z;
+    case LINEAR_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
+    case LINEAR_ACT_GELU_TANH: {
+      const float u = kTanhScale * (z + kTanhCubic * z * z * z);
+      return z / (1.0f + expf(-2.0f * u));
+    }
+    case LINEAR_ACT_SILU: return z / (1.0f + expf(-z));
+    default: return z;
+  }
+}
+
+// d act'(z) in fp32.
+__device__ inline float act_grad(float d, float z, int act) {
+  switch (act) {
+    case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : d;   // zero also where d is not finite
+    case LINEAR_ACT_GELU:
+      return d * (0.5f * erfcf(-0.7071067811865476f * z) + z * (0.3989422804014327f * expf(-0.5f * z * z)));
+    case LINEAR_ACT_GELU_TANH: {
+      // beyond 16 the slope is 0 or 1 to the last bit, and z^3 could overflow
+      if (z > 16.0f) return d;
+      if (z < -16.0f) return d * 0.0f;
+      const float u = kTanhScale * (z + kTanhCubic * z * z * z);
+      const float s = 1.0f / (1.0f + expf(-2.0f * u));
+      return d * (s + 2.0f * z * s * (1.0f - s) * kTanhScale * (1.0f + 3.0f * kTanhCubic * z * z));
+    }
+    case LINEAR_ACT_SILU: {
+      const float s = 1.0f / (1.0f + expf(-z));
+      return d * (s * (1.0f + z * (1.0f - s)));
+    }
+    default: return d;
+  }
+}
+
+// What follows a product: C = act(product + bias) + residual, Z = product + bias.
+struct Epilogue {
+  const void* bias;       // M values or nullptr
+  const void* residual;   // M x N or nullptr
+  int64_t ldr;
+  void* Z;                // M x N or nullptr
+  int64_t ldz;
+  void* C;
+  int64_t ldc;
+  int act;
+};
+
+// C (M x N, M fastest) = A (M x K) B (K x N).
+struct Product {
+  const void* A;
+  const void* B;
+  int64_t lda, ldb;
+  int M, N, K;            // M, N >= 1
+  int splits;             // workgroups that share a tile's contraction
+  int mtiles, ntiles;
+  float* part;            // splits > 1: [splits][N][M] partial products
+  Epilogue e;
+};
+
+// kVec values m .. of column n of the result (all of them inside it); v holds
+// the product's fp32 sums.
+template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, int n, float* v) {
+  constexpr int V = kVec<T>;
+  float x[V];
+  if (e.bias) {
+    load_vec(static_cast<const T*>(e.bias) + m, x);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += x[i];
+  }
+  if (e.Z) store_vec(static_cast<T*>(e.Z) + (int64_t)n * e.ldz + m, v);
+  if (e.act != LINEAR_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = act_value(v[i], e.act);
+  }
+  if (e.residual) {
+    load_vec(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, x);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += x[i];
+  }
+  store_vec(static_cast<T*>(e.C) + (int64_t)n * e.ldc + m, v);
+}
+
+// The same for one value, where a whole vector would pass the last row.
+template <class T> __device__ inline void finish_one(const Epilogue& e, int m, int n, float v) {
+  if (e.bias) v += (float)static_cast<const T*>(e.bias)[m];
+  if (e.Z) static_cast<T*>(e.Z)[(int64_t)n * e.ldz + m] = (T)v;
+  v = act_value(v, e.act);
+  if (e.residual) v += (float)static_cast<const T*>(e.residual)[(int64_t)n * e.ldr + m];
+  static_cast<T*>(e.C)[(int64_t)n * e.ldc + m] = (T)v;
+}
+
+// linear.hip.  Where A's (B's) contiguous index is the contraction, a_kc (b_kc)
+// is set; its rows are then ld apart, else its contraction indices are.
+int compute_units();
+int64_t product_workspace(int dtype, int64_t M, int64_t N, int64_t K);
+hipError_t launch_product(int dtype, bool a_kc, bool b_kc, Product p, void* workspace, hipStream_t s);
+
+// Argument checks of the C ABI.
+constexpr int64_t kSizeLimit = 1ll << 24;
+constexpr int64_t kElemLimit = 1ll << 40;
+
+inline bool is_type(int dtype) { return dtype == LINEAR_F32 || dtype == LINEAR_BF16 || dtype == LINEAR_F16; }
+inline int64_t type_size(int dtype) { return dtype == LINEAR_F32 ? 4 : 2; }
+
+// 0, or minus the first invalid one of dtype, kn, ci, t (arguments 1 .. 4).
+inline int check_sizes(int dtype, int64_t kn, int64_t ci, int64_t t) {
+  if (!is_type(dtype)) return -1;
+  if (kn < 0 || kn >= kSizeLimit) return -2;
+  if (ci < 0 || ci >= kSizeLimit || kn * ci >= kElemLimit) return -3;
+  if (t < 0 || t >= kSizeLimit || kn * t >= kElemLimit || ci * t >= kElemLimit) return -4;
+  return 0;
+}
+
+inline bool bad_ld(int64_t ld, int64_t extent) { return ld < (extent > 1 ? extent : 1) || ld >= kSizeLimit; }
+
+}  // namespace linear

@@ -1,0 +1,197 @@
+// The layer's gradients: dZ = dO act'(Z) and dbias = dZ 1 in one pass over dO
+// (and Z), then dX = F^T dZ and dF = dZ X^T as two products of linear.hip.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "linear_common.h"
+
+namespace linear {
+namespace {
+
+// dZ and the sums of its rows.  A workgroup owns 32 vectors (128 or 256 rows)
+// of `span` tokens; its eight groups of 32 lanes take every eighth token.  The
+// sums are of the fp32 values, before dZ is rounded.  Bound by memory: one
+// read of dO and Z and one write of dZ.
+template <class T, bool ACT, bool SUM>
+__global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, const T* __restrict__ dO, int64_t lddo,
+                                                    const T* __restrict__ Z, int64_t ldz, int act, T* __restrict__ dZ, int64_t lddz,
+                                                    float* __restrict__ part, T* __restrict__ dbias) {
+  constexpr int V = kVec<T>;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int m = (blockIdx.x * 32 + x) * V;
+  const int lo = blockIdx.y * span, hi = min(t, lo + span);
+  float sum[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+  if (m + V <= kn) {
+#pragma unroll 4
+    for (int n = lo + y; n < hi; n += 8) {
+      float d[V], z[V];
+      load_vec(dO + (int64_t)n * lddo + m, d);
+      if (ACT) {
+        load_vec(Z + (int64_t)n * ldz + m, z);
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = act_grad(d[i], z[i], act);
+        store_vec(dZ + (int64_t)n * lddz + m, d);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] += d[i];
+    }
+  } else if (m < kn) {
+    for (int n = lo + y; n < hi; n += 8) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (m + i >= kn) continue;
+        float d = (float)dO[(int64_t)n * lddo + m + i];
+        if (ACT) {
+          d = act_grad(d, (float)Z[(int64_t)n * ldz + m + i], act);
+          dZ[(int64_t)n * lddz + m + i] = (T)d;
+        }
+        sum[i] += d;
+      }
+    }
+  }
+  if (!SUM) return;
+  __shared__ float sh[8][32 * V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sh[y][x * V + i] = sum[i];
+  __syncthreads();
+  for (int r = threadIdx.x; r < 32 * V; r += 256) {
+    const int k = blockIdx.x * 32 * V + r;
+    if (k >= kn) break;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sh[i][r];
+    if (part)
+      part[(int64_t)blockIdx.y * kn + k] = s;
+    else
+      dbias[k] = (T)s;
+  }
+}
+
+template <class T> __global__ __launch_bounds__(256) void bias_kernel(int kn, int parts, const float* part, T* dbias) {
+  const int k = blockIdx.x * 256 + threadIdx.x;
+  if (k >= kn) return;
+  float s = 0.0f;
+  for (int i = 0; i < parts; ++i) s += part[(int64_t)i * kn + k];
+  dbias[k] = (T)s;
+}
+
+// Tokens of one workgroup of slope_kernel: about four workgroups for each
+// compute unit, 32 tokens at least, 256 parts at most.
+int slope_span(int dtype, int64_t kn, int64_t t) {
+  const int64_t width = 32 * 16 / type_size(dtype), cols = (kn + width - 1) / width;
+  const int64_t parts = std::min<int64_t>(256, std::max<int64_t>(1, 4 * compute_units() / std::max<int64_t>(cols, 1)));
+  return (int)std::max<int64_t>(32, (t + parts - 1) / parts);
+}
+
+// The workspace, in order.
+struct Layout {
+  int64_t lddz = 0;            // dZ (act only): kn rounded up to whole vectors
+  int64_t part = 0;            // byte offset of the partial dbias
+  int span = 0, parts = 0;
+  int64_t product = 0;         // byte offset of the products' workspace
+  int64_t bytes = 0;
+};
+
+Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act) {
+  auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+  Layout w;
+  if (act != LINEAR_ACT_NONE) {
+    w.lddz = (kn + 7) / 8 * 8;
+    w.part = up(w.lddz * t * type_size(dtype));
+  }
+  w.span = slope_span(dtype, kn, t);
+  w.parts = (int)((t + w.span - 1) / w.span);
+  w.product = w.part + (w.parts > 1 ? up((int64_t)w.parts * kn * 4) : 0);
+  w.bytes = w.product + std::max(product_workspace(dtype, ci, t, kn),
+                                 f_order ? product_workspace(dtype, ci, kn, t) : product_workspace(dtype, kn, ci, t));
+  return w;
+}
+
+template <class T> hipError_t launch_slope(int64_t kn, int64_t t, const Layout& w, const void* dO, int64_t lddo, const void* Z,
+                                           int64_t ldz, int act, char* ws, void* dbias, hipStream_t s) {
+  const dim3 grid((unsigned)((kn + 32 * kVec<T> - 1) / (32 * kVec<T>)), (unsigned)std::max(1, w.parts));
+  auto k = act == LINEAR_ACT_NONE ? slope_kernel<T, false, true> : dbias ? slope_kernel<T, true, true> : slope_kernel<T, true, false>;
+  float* part = w.parts > 1 ? reinterpret_cast<float*>(ws + w.part) : nullptr;
+  k<<<grid, 256, 0, s>>>((int)kn, (int)t, w.span, static_cast<const T*>(dO), lddo, static_cast<const T*>(Z), ldz, act,
+                         reinterpret_cast<T*>(ws), w.lddz, part, static_cast<T*>(dbias));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !dbias || !part) return e;
+  bias_kernel<T><<<dim3((unsigned)((kn + 255) / 256)), 256, 0, s>>>((int)kn, w.parts, part, static_cast<T*>(dbias));
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace linear
+
+extern "C" int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act) {
+  if (int e = linear::check_sizes(dtype, kn, ci, t)) return e;
+  if (f_order != 0 && f_order != 1) return -5;
+  if (act < LINEAR_ACT_NONE || act > LINEAR_ACT_SILU) return -6;
+  return linear::layout(dtype, kn, ci, t, f_order, act).bytes;
+}
+
+extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order, int64_t ldf,
+                                        const void* X, int64_t ldx, const void* dO, int64_t lddo, const void* Z, int64_t ldz,
+                                        int act, void* dX, int64_t lddx, void* dF, int64_t lddf, void* dbias, void* workspace,
+                                        int64_t workspace_bytes, hipStream_t stream) {
+  using namespace linear;
+  if (int e = check_sizes(dtype, kn, ci, t)) return e;
+  if (!F && dX && kn > 0 && ci > 0 && t > 0) return -5;
+  if (f_order != 0 && f_order != 1) return -6;
+  if (dX && bad_ld(ldf, f_order ? ci : kn)) return -7;
+  if (!X && dF && kn > 0 && ci > 0 && t > 0) return -8;
+  if (dF && bad_ld(ldx, ci)) return -9;
+  if (!dO && kn > 0 && t > 0) return -10;
+  if (bad_ld(lddo, kn)) return -11;
+  if (act < LINEAR_ACT_NONE || act > LINEAR_ACT_SILU) return -14;
+  if (act != LINEAR_ACT_NONE && !Z && kn > 0 && t > 0) return -12;
+  if (act != LINEAR_ACT_NONE && bad_ld(ldz, kn)) return -13;
+  if (dX && bad_ld(lddx, ci)) return -16;
+  if (dF && bad_ld(lddf, f_order ? ci : kn)) return -18;
+  const Layout w = layout(dtype, kn, ci, t, f_order, act);
+  if (w.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return -20;
+  if (workspace_bytes < w.bytes) return -21;
+  char* ws = static_cast<char*>(workspace);
+  hipError_t e = hipSuccess;
+  if (kn > 0 && (dbias || (act != LINEAR_ACT_NONE && t > 0))) {
+    switch (dtype) {
+      case LINEAR_F32: e = launch_slope<float>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream); break;
+      case LINEAR_BF16: e = launch_slope<bf16>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream); break;
+      default: e = launch_slope<f16>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream);
+    }
+  }
+  const void* dZ = act == LINEAR_ACT_NONE ? dO : workspace;
+  const int64_t lddz = act == LINEAR_ACT_NONE ? lddo : w.lddz;
+  if (e == hipSuccess && dX) {
+    Product p{};
+    p.A = F;
+    p.lda = ldf;
+    p.B = dZ;
+    p.ldb = lddz;
+    p.M = (int)ci;
+    p.N = (int)t;
+    p.K = (int)kn;
+    p.e.C = dX;
+    p.e.ldc = lddx;
+    e = launch_product(dtype, f_order == 0, true, p, ws + w.product, stream);
+  }
+  if (e == hipSuccess && dF) {
+    // dF with kn fastest is dZ X^T; with ci fastest its transpose X dZ^T
+    Product p{};
+    p.A = f_order ? X : dZ;
+    p.lda = f_order ? ldx : lddz;
+    p.B = f_order ? dZ : X;
+    p.ldb = f_order ? lddz : ldx;
+    p.M = (int)(f_order ? ci : kn);
+    p.N = (int)(f_order ? kn : ci);
+    p.K = (int)t;
+    p.e.C = dF;
+    p.e.ldc = lddf;
+    e = launch_product(dtype, false, false, p, ws + w.product, stream);
+  }
+  return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
+}

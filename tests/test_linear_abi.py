@@ -1,0 +1,125 @@
+"""Argument checks of the layer operators' C ABI (``include/linear.h``), which
+come before any GPU work, and the plain forms the GPU tests rest on.  No compute
+call is made here (no GPU needed)."""
+from __future__ import annotations
+
+import ctypes
+import math
+import os
+
+import numpy as np
+import pytest
+
+import layer_truths as lt64
+import paper_2005_06410_amd as lt
+from paper_2005_06410_amd import build as ltbuild
+
+BF16, F16, F32 = 4, 5, 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(lt.LIB_PATH):
+        ltbuild.build()
+    return lt.load()
+
+
+GOOD = dict(dtype=F32, kn=4, ci=3, t=2, F=16, order=0, ldf=4, X=16, ldx=3, bias=None, act=0, R=None, ldr=0, Z=None, ldz=0,
+            O=16, ldo=4, ws=16, bytes=1 << 40, stream=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    ({"dtype": 0}, -1), ({"dtype": 2}, -1), ({"kn": -1}, -2), ({"kn": 1 << 24}, -2), ({"ci": -1}, -3), ({"ci": 1 << 24}, -3),
+    ({"kn": 1 << 23, "ci": 1 << 23}, -3), ({"t": -1}, -4), ({"t": 1 << 24}, -4), ({"kn": 1 << 23, "ldf": 1 << 23, "t": 1 << 20}, -4),
+    ({"F": None}, -5), ({"order": 2}, -6), ({"ldf": 3}, -7), ({"order": 1, "ldf": 2}, -7), ({"ldf": 1 << 24}, -7),
+    ({"X": None}, -8), ({"ldx": 2}, -9), ({"act": -1}, -11), ({"act": 5}, -11), ({"R": 16, "ldr": 3}, -13),
+    ({"Z": 16, "ldz": 3}, -15), ({"O": None}, -16), ({"ldo": 3}, -17),
+    ({"t": 0, "F": None, "X": None, "O": None}, 0), ({"kn": 0, "ldf": 1, "ldo": 1, "F": None, "O": None}, 0),
+    # a split contraction needs its workspace
+    ({"kn": 64, "ci": 65536, "ldf": 64, "ldx": 65536, "ldo": 64, "ws": None}, -18),
+    ({"kn": 64, "ci": 65536, "ldf": 64, "ldx": 65536, "ldo": 64, "ws": 24}, -18),
+    ({"kn": 64, "ci": 65536, "ldf": 64, "ldx": 65536, "ldo": 64, "bytes": 15}, -19),
+])
+def test_linear_argument_checks(lib, change, code):
+    a = dict(GOOD, **change)
+    assert lib.convgemm_linear(*a.values()) == code
+
+
+BACK = dict(dtype=F32, kn=4, ci=3, t=2, F=16, order=0, ldf=4, X=16, ldx=3, dO=16, lddo=4, Z=None, ldz=0, act=0, dX=16, lddx=3,
+            dF=16, lddf=4, db=16, ws=16, bytes=1 << 40, stream=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    ({"dtype": 3}, -1), ({"kn": -1}, -2), ({"ci": -1}, -3), ({"t": -1}, -4), ({"F": None}, -5), ({"order": -1}, -6), ({"ldf": 3}, -7),
+    ({"X": None}, -8), ({"ldx": 2}, -9), ({"dO": None}, -10), ({"lddo": 3}, -11), ({"act": 2}, -12), ({"act": 2, "Z": 16, "ldz": 3}, -13),
+    ({"act": 5}, -14), ({"lddx": 2}, -16), ({"lddf": 3}, -18), ({"order": 1, "ldf": 3, "lddf": 2}, -18),
+    ({"act": 2, "Z": 16, "ldz": 4, "ws": None}, -20), ({"act": 2, "Z": 16, "ldz": 4, "ws": 8}, -20),
+    ({"act": 2, "Z": 16, "ldz": 4, "bytes": 8}, -21),
+    ({"kn": 0, "ci": 0, "t": 0, "ldf": 1, "ldx": 1, "lddo": 1, "lddx": 1, "lddf": 1}, 0),
+])
+def test_backward_argument_checks(lib, change, code):
+    a = dict(BACK, **change)
+    assert lib.convgemm_linear_backward(*a.values()) == code
+
+
+def test_workspace_queries(lib):
+    assert lib.convgemm_linear_workspace(F32, 0, 5, 5, 0) == 0
+    assert lib.convgemm_linear_workspace(9, 4, 4, 4, 0) == -1
+    assert lib.convgemm_linear_workspace(F32, 4, 4, 4, 2) == -5
+    assert lib.convgemm_linear_backward_workspace(F32, 4, 4, 4, 0, 5) == -6
+    assert lib.convgemm_linear_backward_workspace(BF16, 100, 50, 30, 1, 2) >= 100 * 30 * 2
+    assert lib.convgemm_grad_workspace(-1) == -1
+    assert 0 < lib.convgemm_grad_workspace(1) <= lib.convgemm_grad_workspace(1000)
+
+
+def arrays(n=(4, 4), dtype=(F32, BF16), ptr=(16, 32)):
+    return ((ctypes.c_void_p * 2)(*ptr), (ctypes.c_int64 * 2)(*n), (ctypes.c_int * 2)(*dtype))
+
+
+@pytest.mark.parametrize("kw,at,code", [
+    ({"n": (4, -1)}, 3, 0), ({"n": (4, 1 << 37)}, 3, 0), ({"dtype": (F32, 0)}, 4, 0), ({"ptr": (16, 0)}, 2, 0),
+])
+def test_grad_list_checks(lib, kw, at, code):
+    g, n, d = arrays(**kw)
+    assert lib.convgemm_grad_norm(2, g, n, d, 16, 16, 1 << 30, None) == -at
+    assert lib.convgemm_grad_clip(2, g, g, n, d, 1.0, 16, 16, 1 << 30, None) == -(at if at == 2 else at + 1)
+
+
+def test_grad_argument_checks(lib):
+    g, n, d = arrays()
+    norm, clip = lib.convgemm_grad_norm, lib.convgemm_grad_clip
+    assert norm(-1, g, n, d, 16, 16, 1 << 30, None) == -1 and clip(-1, g, g, n, d, 1.0, 16, 16, 1 << 30, None) == -1
+    assert norm(2, None, n, d, 16, 16, 1 << 30, None) == -2 and norm(2, g, None, d, 16, 16, 1 << 30, None) == -3
+    assert norm(2, g, n, None, 16, 16, 1 << 30, None) == -4 and norm(2, g, n, d, None, 16, 1 << 30, None) == -5
+    assert norm(2, g, n, d, 16, None, 1 << 30, None) == -6 and norm(2, g, n, d, 16, 8, 1 << 30, None) == -6
+    assert norm(2, g, n, d, 16, 16, 15, None) == -7
+    assert clip(2, g, None, n, d, 1.0, 16, 16, 1 << 30, None) == -3
+    assert clip(2, g, arrays(ptr=(16, 0))[0], n, d, 1.0, 16, 16, 1 << 30, None) == -3
+    for bad in (-1.0, math.nan):
+        assert clip(2, g, g, n, d, bad, 16, 16, 1 << 30, None) == -6
+    assert clip(2, g, g, n, d, 1.0, None, 16, 1 << 30, None) == -7
+    assert clip(2, g, g, n, d, 1.0, 16, 8, 1 << 30, None) == -8 and clip(2, g, g, n, d, 1.0, 16, 16, 15, None) == -9
+
+
+@pytest.mark.parametrize("act", lt64.ACTS)
+def test_plain_slopes_are_the_values_derivatives(act):
+    z = np.linspace(-5, 5, 401) + 0.003          # off relu's corner
+    h = 1e-6
+    want = (lt64.value(z + h, act) - lt64.value(z - h, act)) / (2 * h)
+    assert np.abs(lt64.slope(z, act) - want).max() < 1e-8
+
+
+def test_plain_backward_is_the_gradient():
+    r = np.random.default_rng(3)
+    F, X, dO = r.standard_normal((4, 3)), r.standard_normal((3, 2)), r.standard_normal((4, 2))
+    z = F @ X
+    dX, dF, db, _ = lt64.backward(F, X, dO, z, "silu")
+    h = 1e-6
+    for at in np.ndindex(F.shape):
+        up = F.copy()
+        up[at] += h
+        assert abs(((lt64.linear(up, X, None, "silu", None)[0] - lt64.linear(F, X, None, "silu", None)[0]) * dO).sum() / h
+                   - dF[at]) < 1e-4
+    up = lt64.linear(F, X, np.full(4, h), "silu", None)[0]
+    assert abs(((up - lt64.linear(F, X, None, "silu", None)[0]) * dO).sum() / h - db.sum()) < 1e-4
+    assert dX.shape == X.shape
