@@ -35,8 +35,9 @@
  * first extent.  F and dF have either index fastest, by f_order: 0 = kn fastest
  * (the convolution's filters: F[k][c] at F[k + ldf c]), 1 = ci fastest (F[k][c]
  * at F[c + ldf k]).  Any leading dimension and any address that the type
- * allows are taken; the fast loads need 16-byte aligned addresses and leading
- * dimensions and a contiguous extent that is a multiple of 16 bytes.
+ * allows are taken; operands whose addresses, leading dimensions or contiguous
+ * extents are not multiples of 16 bytes cost narrower loads (fp32), a padded copy
+ * (16-bit types) or, up to 64 tokens, loads through registers.
  *
  * Rules (as in ltlt.h): pointers are DEVICE pointers of the current HIP device
  * unless marked HOST; calls are stream-ordered and asynchronous; the caller
@@ -73,8 +74,21 @@ extern "C" {
 
 /* Bytes of workspace that convgemm_linear needs for a layer of these sizes on
  * the current device (0 where none; host only), or -i when argument i is
- * invalid. */
-int64_t convgemm_linear_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order);
+ * invalid.  aligned = 1 says that F and X have 16-byte aligned addresses and
+ * leading dimensions of whole 16 bytes, below 2^22 bytes; what 0 gives is enough
+ * for any. */
+int64_t convgemm_linear_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int aligned);
+
+/* The kernel that convgemm_linear takes for a layer on the current device (host
+ * only; without a device, on one of 256 CUs; `aligned` as above).  HOST int
+ * out[5]:
+ *   out[0] = 1 the 256 x 256 tile's kernel, 2 a kernel with another tile, 3 one
+ *            that loads single fp32 values, 4 loads through registers; 0 where
+ *            there is nothing to do;
+ *   out[1], out[2] = its tile, outputs x tokens;
+ *   out[3] = workgroups that share a tile's contraction (added in a fixed order);
+ *   out[4] = operands that are copied first. */
+int convgemm_linear_choice(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int aligned, int* out);
 
 /* O = act(F X + bias) + residual.
  *   dtype             : LINEAR_*;
@@ -95,8 +109,9 @@ int convgemm_linear(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F,
                     hipStream_t stream);
 
 /* Bytes of workspace that convgemm_linear_backward needs (host only), or -i
- * when argument i is invalid. */
-int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act);
+ * when argument i is invalid.  aligned: as above, of F, X and dO. */
+int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act,
+                                           int aligned);
 
 /* dX, dF and dbias from dO; each of the three may be NULL and is then not
  * computed.  F may be NULL where dX is, X where dF is.  Z is the pre-activation

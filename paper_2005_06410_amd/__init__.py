@@ -24,7 +24,10 @@ call since the previous ``device_status()`` failed.
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import functools
+import operator
 import os
 import threading
 
@@ -91,12 +94,13 @@ _SYMBOLS = {
     "convgemm_f32": ([ctypes.c_int] * 9 + [ctypes.c_void_p] * 3 + [ctypes.c_int] * 4 + [ctypes.c_void_p],
                      ctypes.c_int),
     # include/linear.h
-    "convgemm_linear_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int], ctypes.c_int64),
+    "convgemm_linear_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 2, ctypes.c_int64),
+    "convgemm_linear_choice": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 2 + [ctypes.c_void_p], ctypes.c_int),
     "convgemm_linear": ([ctypes.c_int] + [ctypes.c_int64] * 3
                         + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
                            ctypes.c_void_p, ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int64] * 4
                         + [ctypes.c_void_p], ctypes.c_int),
-    "convgemm_linear_backward_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 2, ctypes.c_int64),
+    "convgemm_linear_backward_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 3, ctypes.c_int64),
     "convgemm_linear_backward": ([ctypes.c_int] + [ctypes.c_int64] * 3
                                  + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64]
                                  + [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_int]
@@ -132,6 +136,8 @@ class LtltError(RuntimeError):
 def load():
     """Load ``libltlt.so`` (raises if it has not been built)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -152,9 +158,15 @@ def _check(fn: str, code: int):
         raise LtltError(fn, code)
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -444,19 +456,20 @@ def convgemm(F, I, stride: int = 1, pad: int = 0, out=None, accumulate: bool = F
     return out
 
 
-# Layer operators (include/linear.h).
+# Layer operators (include/linear.h).  A call of a few tokens is bound by what
+# happens on the host, so these bindings ask each tensor each thing once.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-_layer_codes = None
+_layer_codes = {}
 
 
-def _layer_dtype(t) -> int:
-    global _layer_codes
-    if _layer_codes is None:
-        torch = _torch()
-        _layer_codes = {torch.float32: 1, torch.bfloat16: 4, torch.float16: 5}
-    code = _layer_codes.get(t.dtype)
+def _layer_dtype(dtype) -> int:
+    code = _layer_codes.get(dtype)
     if code is None:
-        raise TypeError("only float32, bfloat16 and float16 are supported")
+        torch = _torch()
+        _layer_codes.update({torch.float32: 1, torch.bfloat16: 4, torch.float16: 5})
+        code = _layer_codes.get(dtype)
+        if code is None:
+            raise TypeError("only float32, bfloat16 and float16 are supported")
     return code
 
 
@@ -467,47 +480,88 @@ def _activation(name) -> int:
     return code
 
 
-def _columns(t, rows: int, cols: int, name: str, like) -> int:
+def _layer_input(X):
+    """(ci, t, leading dimension, dtype, its code, GPU index) of a layer's input."""
+    _require_gpu(X)
+    if X.dim() != 2:
+        raise ValueError("X must be (ci, t)")
+    ci, t = X.shape
+    dtype, dev = X.dtype, X.get_device()
+    return ci, t, _columns(X, ci, t, "X", dtype, dev), dtype, _layer_dtype(dtype), dev
+
+
+def _columns(v, rows: int, cols: int, name: str, dtype, dev: int) -> int:
     """The leading dimension of a (rows, cols) tensor stored with its first
-    index fastest, of `like`'s dtype and device."""
-    if tuple(t.shape) != (rows, cols):
+    index fastest, of the given dtype on the given GPU."""
+    if v.shape != (rows, cols):
         raise ValueError(f"{name} must have shape {(rows, cols)}")
-    if t.dtype != like.dtype:
+    if v.dtype != dtype:
         raise TypeError(f"{name} must have X's dtype")
-    if t.device != like.device:
+    if v.get_device() != dev:
         raise ValueError("all tensor arguments must be on the same GPU")
-    s0, s1 = t.stride()
+    s0, s1 = v.stride()
     if (rows > 1 and s0 != 1) or (cols > 1 and s1 < max(rows, 1)):
         raise ValueError(f"{name} must be stored leftmost index fastest: stride(0) == 1, stride(1) >= {rows}")
     return s1 if cols > 1 else max(rows, 1)
 
 
-def _weights(F, like):
-    """(kn, ci, order, leading dimension) of weights with either index fastest."""
+def _weights(F, ci: int, dtype, dev: int):
+    """(kn, order, leading dimension) of weights with either index fastest."""
     if F.dim() != 2:
         raise ValueError("F must be (kn, ci)")
-    if F.dtype != like.dtype:
+    if F.dtype != dtype:
         raise TypeError("F must have X's dtype")
-    if F.device != like.device:
+    if F.get_device() != dev:
         raise ValueError("all tensor arguments must be on the same GPU")
-    kn, ci = F.shape
+    kn, fci = F.shape
+    if fci != ci:
+        raise ValueError("F and X disagree on the number of inputs")
     s0, s1 = F.stride()
     if (ci <= 1 or s1 == 1) and (kn <= 1 or s0 >= max(ci, 1)):
-        return kn, ci, 1, s0 if kn > 1 else max(ci, 1)
+        return kn, 1, s0 if kn > 1 else max(ci, 1)
     if (kn <= 1 or s0 == 1) and (ci <= 1 or s1 >= max(kn, 1)):
-        return kn, ci, 0, s1 if ci > 1 else max(kn, 1)
+        return kn, 0, s1 if ci > 1 else max(kn, 1)
     raise ValueError("F must have one index with stride 1 and no overlap along the other")
 
 
-def _on_device(t):
-    """Makes t's GPU the current one for a call."""
-    import contextlib
+def _aligned(code: int, lds: int, ptrs: int) -> int:
+    """Whether leading dimensions (or-ed together) and addresses (likewise) are
+    whole 16 bytes, and the former below the direct loads' limit."""
+    size = 4 if code == 1 else 2
+    return int(not (lds * size | ptrs) & 15 and lds < 1 << 20)
+
+
+def _raw_stream(dev: int) -> int:
+    """The current stream of GPU `dev`, by torch's direct query where it has one."""
+    c = _torch()._C
+    raw = getattr(c, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw is not None else _stream_ptr(dev)
+
+
+@functools.lru_cache(maxsize=4096)
+def _scratch_bytes(fn: str, dev: int, *sizes) -> int:
+    """What the library answers for these sizes on GPU `dev`."""
+    with _torch().cuda.device(dev):
+        need = getattr(load(), fn)(*sizes)
+    if need < 0:
+        raise ValueError(f"sizes out of range (argument {-need} of {fn})")
+    return need
+
+
+def _scratch(need: int, like):
+    """Workspace of a call, from torch's allocator: stream-ordered like the call."""
+    return like.new_empty(need, dtype=_torch().uint8)
+
+
+def _launch(fn: str, dev: int, *args):
+    """Calls the library with the current stream, on the tensors' GPU."""
     torch = _torch()
-    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-
-def _new_columns(rows: int, cols: int, like):
-    return _torch().empty((cols, rows), dtype=like.dtype, device=like.device).t()
+    f = getattr(load(), fn)
+    if torch.cuda.current_device() == dev:
+        _check(fn, f(*args, _raw_stream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn, f(*args, _raw_stream(dev)))
 
 
 def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, keep_pre: bool = False):
@@ -524,42 +578,47 @@ def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, k
     Returns O (kn, t) in the same storage (``out`` if given; it may be
     ``residual`` itself), or (O, Z) with the pre-activation
     Z = F X + bias for ``linear_backward`` where ``keep_pre`` is set."""
-    _require_gpu(X)
-    if X.dim() != 2:
-        raise ValueError("X must be (ci, t)")
-    code, act = _layer_dtype(X), _activation(activation)
-    kn, ci, order, ldf = _weights(F, X)
-    t = X.shape[1]
-    ldx = _columns(X, ci, t, "X", X)
-    bp = 0
+    ci, t, ldx, dtype, code, dev = _layer_input(X)
+    kn, order, ldf = _weights(F, ci, dtype, dev)
+    act = _activation(activation)
+    bp = rp = zp = 0
+    ldr = 1
     if bias is not None:
         if bias.shape != (kn,) or (kn > 1 and bias.stride(0) != 1):
             raise ValueError(f"bias must be a contiguous tensor of {kn} values")
-        if bias.dtype != X.dtype:
+        if bias.dtype != dtype:
             raise TypeError("bias must have X's dtype")
-        _same_device(X, bias)
+        if bias.get_device() != dev:
+            raise ValueError("all tensor arguments must be on the same GPU")
         bp = bias.data_ptr()
-    rp, ldr = (0, 1) if residual is None else (residual.data_ptr(), _columns(residual, kn, t, "residual", X))
+    if residual is not None:
+        ldr = _columns(residual, kn, t, "residual", dtype, dev)
+        rp = residual.data_ptr()
     if out is None:
-        out = _new_columns(kn, t, X)
-    ldo = _columns(out, kn, t, "out", X)
-    Z = _new_columns(kn, t, X) if keep_pre else None
-    lib = load()
-    with _on_device(X):
-        need = lib.convgemm_linear_workspace(code, kn, ci, t, order)
-        ws = _workspace(need, X.device)
-        err = lib.convgemm_linear(code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, bp, act, rp, ldr,
-                                  Z.data_ptr() if keep_pre else 0, max(kn, 1), out.data_ptr(), ldo,
-                                  0 if ws is None else ws.data_ptr(), need, _stream_ptr(X.device))
-    _check("convgemm_linear", err)
+        out = X.new_empty_strided((kn, t), (1, max(kn, 1)))
+        ldo = max(kn, 1)
+    else:
+        ldo = _columns(out, kn, t, "out", dtype, dev)
+    if keep_pre:
+        Z = X.new_empty_strided((kn, t), (1, max(kn, 1)))
+        zp = Z.data_ptr()
+    fp, xp = F.data_ptr(), X.data_ptr()
+    need = _scratch_bytes("convgemm_linear_workspace", dev, code, kn, ci, t, order,
+                          _aligned(code, ldf | ldx, fp | xp))
+    ws = _scratch(need, X) if need else None
+    _launch("convgemm_linear", dev, code, kn, ci, t, fp, order, ldf, xp, ldx, bp, act, rp, ldr, zp,
+            max(kn, 1), out.data_ptr(), ldo, ws.data_ptr() if need else 0, need)
     return (out, Z) if keep_pre else out
 
 
-def _workspace(need: int, device):
-    """Scratch of a call, from torch's allocator: stream-ordered like the call."""
-    if need < 0:
-        raise ValueError(f"sizes out of range (argument {-need} of the layer)")
-    return _torch().empty(need, dtype=_torch().uint8, device=device) if need else None
+def linear_choice(dtype, kn: int, ci: int, t: int, f_order: int = 1, aligned: bool = True):
+    """The kernel that ``linear`` takes for a layer, as (family, tile outputs,
+    tile tokens, splits, copies): see ``convgemm_linear_choice``.  Host only;
+    ``f_order`` 1 for row-major weights, 0 for the convolution's order."""
+    out = (ctypes.c_int * 5)()
+    _check("convgemm_linear_choice", load().convgemm_linear_choice(
+        _layer_dtype(dtype), int(kn), int(ci), int(t), int(f_order), int(bool(aligned)), ctypes.addressof(out)))
+    return tuple(out)
 
 
 def linear_backward(F, X, dO, pre=None, activation: str = "none", needs=(True, True, True)):
@@ -569,37 +628,33 @@ def linear_backward(F, X, dO, pre=None, activation: str = "none", needs=(True, T
     ``pre`` is the Z that ``linear(..., keep_pre=True)`` returned; without an
     activation it is not needed.  dX is stored like X, dF in F's order.
     ``needs`` leaves out what is not wanted (None is returned in its place)."""
-    _require_gpu(X)
-    if X.dim() != 2:
-        raise ValueError("X must be (ci, t)")
-    code, act = _layer_dtype(X), _activation(activation)
-    kn, ci, order, ldf = _weights(F, X)
-    t = X.shape[1]
-    ldx = _columns(X, ci, t, "X", X)
-    lddo = _columns(dO, kn, t, "dO", X)
+    ci, t, ldx, dtype, code, dev = _layer_input(X)
+    kn, order, ldf = _weights(F, ci, dtype, dev)
+    act = _activation(activation)
+    lddo = _columns(dO, kn, t, "dO", dtype, dev)
     zp, ldz = 0, 1
     if act:
         if pre is None:
             raise ValueError("an activation's gradient needs the pre-activation (pre)")
-        zp, ldz = pre.data_ptr(), _columns(pre, kn, t, "pre", X)
-    torch = _torch()
-    dX = _new_columns(ci, t, X) if needs[0] else None
-    dF = (torch.empty((kn, ci), dtype=X.dtype, device=X.device) if order else _new_columns(kn, ci, X)) if needs[1] else None
-    dbias = torch.empty(kn, dtype=X.dtype, device=X.device) if needs[2] else None
-    lib = load()
-
-    def ptr(v):
-        return 0 if v is None else v.data_ptr()
-
-    with _on_device(X):
-        need = lib.convgemm_linear_backward_workspace(code, kn, ci, t, order, act)
-        ws = _workspace(need, X.device)
-        err = lib.convgemm_linear_backward(code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, dO.data_ptr(),
-                                           lddo, zp, ldz, act, ptr(dX), max(ci, 1), ptr(dF),
-                                           max(ci if order else kn, 1), ptr(dbias), ptr(ws), need,
-                                           _stream_ptr(X.device))
-    _check("convgemm_linear_backward", err)
-    return dX, dF, dbias
+        ldz = _columns(pre, kn, t, "pre", dtype, dev)
+        zp = pre.data_ptr()
+    dX = dF = db = None
+    xp = fp = bp = 0
+    if needs[0]:
+        dX = X.new_empty_strided((ci, t), (1, max(ci, 1)))
+        xp = dX.data_ptr()
+    if needs[1]:
+        dF = X.new_empty_strided((kn, ci), (max(ci, 1), 1) if order else (1, max(kn, 1)))
+        fp = dF.data_ptr()
+    if needs[2]:
+        db = X.new_empty(kn)
+        bp = db.data_ptr()
+    need = _scratch_bytes("convgemm_linear_backward_workspace", dev, code, kn, ci, t, order, act,
+                          _aligned(code, ldf | ldx | lddo, F.data_ptr() | X.data_ptr() | dO.data_ptr()))
+    ws = _scratch(need, X) if need else None
+    _launch("convgemm_linear_backward", dev, code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, dO.data_ptr(),
+            lddo, zp, ldz, act, xp, max(ci, 1), fp, max(ci if order else kn, 1), bp, ws.data_ptr() if need else 0, need)
+    return dX, dF, db
 
 
 def _dense(t) -> bool:
@@ -615,22 +670,25 @@ def _dense(t) -> bool:
 
 
 def _grad_list(grads, what):
-    import array
+    """(tensors, GPU index, whether all are contiguous, and as host arrays their
+    addresses, sizes and types); one C-level pass over the list per question."""
     grads = list(grads)
-    dev = None
-    ptrs, sizes, codes = array.array("Q"), array.array("q"), array.array("i")
-    for g in grads:
-        if dev is None:
-            _require_gpu(g)
-            dev = g.device
-        elif g.device != dev:
-            raise ValueError(f"all {what} must be on the same GPU")
-        if not _dense(g):
-            raise ValueError(f"{what} must be stored without gaps or overlap")
-        ptrs.append(g.data_ptr())
-        sizes.append(g.numel())
-        codes.append(_layer_dtype(g))
-    return grads, dev, ptrs, sizes, codes
+    if not grads:
+        raise ValueError(f"no {what}")
+    T = _torch().Tensor
+    devs = set(map(T.get_device, grads))
+    dev = devs.pop()
+    if dev < 0 or devs:
+        raise ValueError(f"all {what} must be on the same GPU (the library has no CPU path)")
+    plain = all(map(T.is_contiguous, grads))
+    if not plain and not all(map(_dense, grads)):
+        raise ValueError(f"{what} must be stored without gaps or overlap")
+    dtypes = list(map(operator.attrgetter("dtype"), grads))
+    if dtypes.count(dtypes[0]) == len(dtypes):
+        codes = array.array("i", (_layer_dtype(dtypes[0]),)) * len(grads)
+    else:
+        codes = array.array("i", map(_layer_dtype, dtypes))
+    return grads, dev, plain, array.array("Q", map(T.data_ptr, grads)), array.array("q", map(T.numel, grads)), codes
 
 
 def grad_norm(grads):
@@ -645,7 +703,7 @@ def grad_norm(grads):
 def clip_grad_norm(grads, max_norm: float, out=None):
     """Scales ``grads`` by c = min(1, max_norm / norm) with their joint norm
     (``convgemm_grad_clip``), in place or into the tensors ``out`` (the same
-    shapes, types and strides).  Returns the norm before scaling, as
+    sizes, types and order in memory).  Returns the norm before scaling, as
     ``grad_norm`` does; nothing is copied to the host.
 
     An infinite norm makes c zero and a NaN norm makes it NaN."""
@@ -655,32 +713,23 @@ def clip_grad_norm(grads, max_norm: float, out=None):
 
 
 def _norm_and_clip(grads, max_norm, out):
-    grads, dev, ptrs, sizes, codes = _grad_list(grads, "gradients")
-    if not grads:
-        raise ValueError("no gradients")
+    grads, dev, plain, ptrs, sizes, codes = _grad_list(grads, "gradients")
     optrs = ptrs
     if out is not None:
-        outs, odev, optrs, osizes, ocodes = _grad_list(out, "outputs")
-        if odev != dev or osizes != sizes or ocodes != codes or any(
-                o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))
-                for o, g in zip(outs, grads)):
-            raise ValueError("out must have the gradients' shapes, types, strides and GPU")
-    torch = _torch()
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    lib = load()
+        outs, odev, oplain, optrs, osizes, ocodes = _grad_list(out, "outputs")
+        if odev != dev or osizes != sizes or ocodes != codes or (not (plain and oplain) and any(
+                [o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))
+                 for o, g in zip(outs, grads)])):
+            raise ValueError("out must have the gradients' sizes, types, order in memory and GPU")
+    norm = grads[0].new_empty((), dtype=_torch().float32)
     count = len(grads)
-    need = lib.convgemm_grad_workspace(count)
-    ws = _workspace(need, dev)
-    a = [v.buffer_info()[0] for v in (ptrs, optrs, sizes, codes)]
-    with _on_device(norm):
-        s = _stream_ptr(dev)
-        if max_norm is None:
-            fn = "convgemm_grad_norm"
-            err = lib.convgemm_grad_norm(count, a[0], a[2], a[3], norm.data_ptr(), ws.data_ptr(), need, s)
-        else:
-            fn = "convgemm_grad_clip"
-            err = lib.convgemm_grad_clip(count, a[0], a[1], a[2], a[3], max_norm, norm.data_ptr(), ws.data_ptr(), need, s)
-    _check(fn, err)
+    need = _scratch_bytes("convgemm_grad_workspace", dev, count)
+    ws = _scratch(need, grads[0])
+    g, o, n, d = [v.buffer_info()[0] for v in (ptrs, optrs, sizes, codes)]
+    if max_norm is None:
+        _launch("convgemm_grad_norm", dev, count, g, n, d, norm.data_ptr(), ws.data_ptr(), need)
+    else:
+        _launch("convgemm_grad_clip", dev, count, g, o, n, d, max_norm, norm.data_ptr(), ws.data_ptr(), need)
     return norm
 
 

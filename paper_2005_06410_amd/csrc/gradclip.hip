@@ -9,21 +9,26 @@
 // not depend on which workgroup ends first and no third launch is needed.
 //
 // Bound by memory: 16-byte loads at any alignment, four in flight per thread.
+// The second pass takes each workgroup's run from its end, where the first one
+// left off: what is still in the last-level cache (256 MB) is not read again
+// from HBM.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear_common.h"
 
 namespace linear {
 namespace {
 
-constexpr int kList = 120;          // tensors of one launch: the list travels in the kernel's arguments
+constexpr int kList = 240;          // tensors of one launch: the list travels in the kernel's arguments
 constexpr int64_t kTensorLimit = 1ll << 37;   // values of one tensor: the chunks of a list are below 2^31
 constexpr int kParts = 2048;        // partial sums (workgroups of the first pass)
-constexpr int kChunkBytes = 32768;  // of one step of a workgroup
+constexpr int kMinChunk = 4096;     // bytes that a workgroup takes at a time: one vector per thread ..
+constexpr int kMaxChunk = 32768;    // .. to eight
 
 struct List {
   const void* g[kList];
@@ -32,8 +37,8 @@ struct List {
   int first[kList + 1];             // chunks before each tensor
   unsigned char dtype[kList];
   int count;
+  int chunk;                        // bytes
 };
-static_assert(sizeof(List) < 4000, "the list fits the kernel's arguments");
 
 __device__ inline double block_sum(double v) {
   __shared__ double sh[4];
@@ -55,71 +60,71 @@ __device__ inline int tensor_of(const List& l, int c) {
   return lo;
 }
 
+// Calls f(vectors at hand, first of them) for the n values of a chunk in groups
+// of up to four 16-byte vectors per thread, and g(value) for what is left over.
+template <class T, class F, class G> __device__ inline void for_values(int64_t n, F f, G g) {
+  constexpr int V = kVec<T>;
+  const int whole = (int)(n / V);
+  int i = threadIdx.x;
+  for (; i + 768 < whole; i += 1024) f(std::integral_constant<int, 4>{}, i);
+  for (; i < whole; i += 256) f(std::integral_constant<int, 1>{}, i);
+  const int rest = (int)(n - (int64_t)whole * V);
+  if ((int)threadIdx.x < rest) g(whole * V + (int)threadIdx.x);
+}
+
 template <class T> __device__ inline double squares(const T* g, int64_t n) {
   constexpr int V = kVec<T>;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
-  const int64_t whole = n / V;
-  int64_t i = threadIdx.x;
-  for (; i + 768 < whole; i += 1024) {
-    float v[4][V];
+  for_values<T>(
+      n,
+      [&](auto count, int i) {
+        constexpr int C = decltype(count)::value;
+        float v[C][V];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_vec(g + (i + 256 * u) * V, v[u]);
+        for (int u = 0; u < C; ++u) load_vec(g + (int64_t)(i + 256 * u) * V, v[u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < C; ++u)
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[u] = fma((double)v[u][j], (double)v[u][j], s[u]);
-  }
-  for (; i < whole; i += 256) {
-    float v[V];
-    load_vec(g + i * V, v);
-#pragma unroll
-    for (int j = 0; j < V; ++j) s[j & 3] = fma((double)v[j], (double)v[j], s[j & 3]);
-  }
-  if (threadIdx.x < n - whole * V) {
-    const double x = (double)(float)g[whole * V + threadIdx.x];
-    s[0] = fma(x, x, s[0]);
-  }
+          for (int j = 0; j < V; ++j) s[j & 3] = fma((double)v[u][j], (double)v[u][j], s[j & 3]);
+      },
+      [&](int i) {
+        const double x = (double)(float)g[i];
+        s[0] = fma(x, x, s[0]);
+      });
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 template <class T> __device__ inline void scale(const T* g, T* out, int64_t n, float c) {
   constexpr int V = kVec<T>;
-  const int64_t whole = n / V;
-  int64_t i = threadIdx.x;
-  for (; i + 768 < whole; i += 1024) {
-    float v[4][V];
+  for_values<T>(
+      n,
+      [&](auto count, int i) {
+        constexpr int C = decltype(count)::value;
+        float v[C][V];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_vec(g + (i + 256 * u) * V, v[u]);
+        for (int u = 0; u < C; ++u) load_vec(g + (int64_t)(i + 256 * u) * V, v[u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < C; ++u) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[u][j] *= c;
-      store_vec(out + (i + 256 * u) * V, v[u]);
-    }
-  }
-  for (; i < whole; i += 256) {
-    float v[V];
-    load_vec(g + i * V, v);
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] *= c;
-    store_vec(out + i * V, v);
-  }
-  if (threadIdx.x < n - whole * V) {
-    const int64_t j = whole * V + threadIdx.x;
-    out[j] = (T)((float)g[j] * c);
-  }
+          for (int j = 0; j < V; ++j) v[u][j] *= c;
+          store_vec(out + (int64_t)(i + 256 * u) * V, v[u]);
+        }
+      },
+      [&](int i) { out[i] = (T)((float)g[i] * c); });
 }
 
-// Calls f(tensor, first value, values) for the chunks lo .. hi-1.
-template <class F> __device__ inline void for_chunks(const List& l, int lo, int hi, F f) {
+// Calls f(tensor, first value, values) for the chunks lo .. hi-1, one at a time,
+// from the last one where `back` is set.
+template <bool back, class F> __device__ inline void for_chunks(const List& l, int lo, int hi, F f) {
   if (lo >= hi) return;
-  for (int i = tensor_of(l, lo); lo < hi; ++i) {
-    const int end = min(hi, l.first[i + 1]);
-    if (end <= lo) continue;
-    const int64_t per = kChunkBytes / (l.dtype[i] == LINEAR_F32 ? 4 : 2);
-    const int64_t at = (int64_t)(lo - l.first[i]) * per;
-    f(i, at, min(l.n[i] - at, (int64_t)(end - lo) * per));
-    lo = end;
+  int i = tensor_of(l, back ? hi - 1 : lo);
+  for (int k = 0; k < hi - lo; ++k) {
+    const int c = back ? hi - 1 - k : lo + k;
+    while (c >= l.first[i + 1]) ++i;
+    while (c < l.first[i]) --i;
+    const int64_t per = l.chunk / (l.dtype[i] == LINEAR_F32 ? 4 : 2);
+    const int64_t at = (int64_t)(c - l.first[i]) * per;
+    f(i, at, min(l.n[i] - at, per));
   }
 }
 
@@ -127,7 +132,7 @@ __global__ __launch_bounds__(256) void norm_kernel(List l, double* part) {
   const int chunks = l.first[l.count];
   const int lo = (int)((int64_t)chunks * blockIdx.x / gridDim.x), hi = (int)((int64_t)chunks * (blockIdx.x + 1) / gridDim.x);
   double s = 0.0;
-  for_chunks(l, lo, hi, [&](int i, int64_t at, int64_t n) {
+  for_chunks<false>(l, lo, hi, [&](int i, int64_t at, int64_t n) {
     if (l.dtype[i] == LINEAR_F32)
       s += squares(static_cast<const float*>(l.g[i]) + at, n);
     else if (l.dtype[i] == LINEAR_BF16)
@@ -158,7 +163,7 @@ __global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, 
   const float c = v <= max_norm ? 1.0f : (float)(max_norm / v);
   const int chunks = l.first[l.count];
   const int lo = (int)((int64_t)chunks * blockIdx.x / gridDim.x), hi = (int)((int64_t)chunks * (blockIdx.x + 1) / gridDim.x);
-  for_chunks(l, lo, hi, [&](int i, int64_t at, int64_t n) {
+  for_chunks<true>(l, lo, hi, [&](int i, int64_t at, int64_t n) {
     if (c == 1.0f && l.out[i] == l.g[i]) return;
     if (l.dtype[i] == LINEAR_F32)
       scale(static_cast<const float*>(l.g[i]) + at, static_cast<float*>(l.out[i]) + at, n, c);
@@ -170,12 +175,13 @@ __global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, 
 }
 
 // Fills `l` with tensors from `from` on; returns the next one that did not fit.
-int take(List& l, int from, int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype) {
+int take(List& l, int chunk, int from, int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype) {
   l.count = 0;
   l.first[0] = 0;
+  l.chunk = chunk;
   for (; from < count && l.count < kList; ++from) {
     if (n[from] == 0) continue;
-    const int64_t chunks = (n[from] * type_size(dtype[from]) + kChunkBytes - 1) / kChunkBytes;
+    const int64_t chunks = (n[from] * type_size(dtype[from]) + chunk - 1) / chunk;
     const int i = l.count++;
     l.g[i] = g[from];
     l.out[i] = out ? out[from] : nullptr;
@@ -184,6 +190,16 @@ int take(List& l, int from, int count, const void* const* g, void* const* out, c
     l.first[i + 1] = l.first[i] + (int)chunks;
   }
   return from;
+}
+
+// Bytes of a chunk: as large as leaves every one of the first pass's workgroups
+// a chunk.
+int chunk_of(int count, const int64_t* n, const int* dtype) {
+  int64_t bytes = 0;
+  for (int i = 0; i < count; ++i) bytes += n[i] * type_size(dtype[i]);
+  int chunk = kMinChunk;
+  while (chunk < kMaxChunk && bytes / (2 * chunk) >= kParts) chunk *= 2;
+  return chunk;
 }
 
 unsigned workgroups(const List& l) { return (unsigned)std::min(l.first[l.count], kParts); }
@@ -195,8 +211,9 @@ int run(int count, const void* const* g, void* const* out, const int64_t* n, con
   double* part = static_cast<double*>(workspace);
   int parts = 0;
   List l;
+  const int chunk = chunk_of(count, n, dtype);
   for (int at = 0; at < count;) {
-    at = take(l, at, count, g, out, n, dtype);
+    at = take(l, chunk, at, count, g, out, n, dtype);
     if (l.count == 0) break;
     norm_kernel<<<dim3(workgroups(l)), 256, 0, s>>>(l, part + parts);
     parts += (int)workgroups(l);
@@ -204,7 +221,7 @@ int run(int count, const void* const* g, void* const* out, const int64_t* n, con
   hipError_t e = hipGetLastError();
   bool told = false;
   for (int at = 0; e == hipSuccess && out && at < count;) {
-    at = take(l, at, count, g, out, n, dtype);
+    at = take(l, chunk, at, count, g, out, n, dtype);
     if (l.count == 0) break;
     scale_kernel<<<dim3(workgroups(l)), 256, 0, s>>>(l, part, parts, max_norm, told ? nullptr : norm);
     told = true;

@@ -41,38 +41,65 @@ template <class T> __device__ inline void store_vec(T* p, const float* v) {
 constexpr float kTanhScale = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
 
-// act(z) in fp32.  gelu takes Phi from erfc, which keeps its relative accuracy
-// for negative z; gelu_tanh takes (1 + tanh u) / 2 as the logistic function of
-// 2u, for the same reason.
-__device__ inline float act_value(float z, int act) {
+// exp(x) and 1 / x: to fp32 accuracy for fp32 results; for the 16-bit types by
+// the hardware's approximations, whose error of about 2^-22 is far below the
+// result's rounding.
+template <class T> __device__ inline float exp_of(float x) {
+  return sizeof(T) == 4 ? expf(x) : __builtin_amdgcn_exp2f(1.4426950408889634f * x);
+}
+template <class T> __device__ inline float inverse(float x) { return sizeof(T) == 4 ? 1.0f / x : __builtin_amdgcn_rcpf(x); }
+
+// Phi(z), and in `e` exp(-z^2 / 2).  fp32: from erfc, which keeps its relative
+// accuracy for negative z.  16-bit types: Abramowitz and Stegun's formula 7.1.26
+// (a polynomial in 1 / (1 + p x) times exp(-x^2), |error| <= 1.5e-7), a third of
+// erfc's instructions; the epilogue of a large product is bound by them.
+template <class T> __device__ inline float normal_cdf(float z, float& e) {
+  e = exp_of<T>(-0.5f * z * z);
+  if constexpr (sizeof(T) == 4) return 0.5f * erfcf(-0.7071067811865476f * z);
+  const float x = 0.7071067811865476f * fabsf(z);
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+  const float q = 0.5f * e * t *
+                  (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  return z < 0.0f ? q : 1.0f - q;
+}
+
+// The logistic function of 2u, u = sqrt(2/pi) (z + 0.044715 z^3): (1 + tanh u) / 2
+// without its cancellation for negative u.
+template <class T> __device__ inline float tanh_gate(float z) {
+  const float u = kTanhScale * (z + kTanhCubic * z * z * z);
+  return inverse<T>(1.0f + exp_of<T>(-2.0f * u));
+}
+
+// act(z) in fp32.
+template <class T> __device__ inline float act_value(float z, int act) {
+  float e;
   switch (act) {
     case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-    case LINEAR_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
-    case LINEAR_ACT_GELU_TANH: {
-      const float u = kTanhScale * (z + kTanhCubic * z * z * z);
-      return z / (1.0f + expf(-2.0f * u));
-    }
-    case LINEAR_ACT_SILU: return z / (1.0f + expf(-z));
+    case LINEAR_ACT_GELU: return z * normal_cdf<T>(z, e);
+    case LINEAR_ACT_GELU_TANH: return z * tanh_gate<T>(z);
+    case LINEAR_ACT_SILU: return z * inverse<T>(1.0f + exp_of<T>(-z));
     default: return z;
   }
 }
 
 // d act'(z) in fp32.
-__device__ inline float act_grad(float d, float z, int act) {
+template <class T> __device__ inline float act_grad(float d, float z, int act) {
   switch (act) {
     case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : d;   // zero also where d is not finite
-    case LINEAR_ACT_GELU:
-      return d * (0.5f * erfcf(-0.7071067811865476f * z) + z * (0.3989422804014327f * expf(-0.5f * z * z)));
+    case LINEAR_ACT_GELU: {
+      float e;
+      const float c = normal_cdf<T>(z, e);
+      return d * (c + z * (0.3989422804014327f * e));
+    }
     case LINEAR_ACT_GELU_TANH: {
       // beyond 16 the slope is 0 or 1 to the last bit, and z^3 could overflow
       if (z > 16.0f) return d;
       if (z < -16.0f) return d * 0.0f;
-      const float u = kTanhScale * (z + kTanhCubic * z * z * z);
-      const float s = 1.0f / (1.0f + expf(-2.0f * u));
+      const float s = tanh_gate<T>(z);
       return d * (s + 2.0f * z * s * (1.0f - s) * kTanhScale * (1.0f + 3.0f * kTanhCubic * z * z));
     }
     case LINEAR_ACT_SILU: {
-      const float s = 1.0f / (1.0f + expf(-z));
+      const float s = inverse<T>(1.0f + exp_of<T>(-z));
       return d * (s * (1.0f + z * (1.0f - s)));
     }
     default: return d;
@@ -97,6 +124,8 @@ struct Product {
   const void* B;
   int64_t lda, ldb;
   int M, N, K;            // M, N >= 1
+  int arows, aK;          // extents of the operands as they are loaded: M and K
+  int brows, bK;          // (N and K), or more where zeros follow
   int splits;             // workgroups that share a tile's contraction
   int mtiles, ntiles;
   float* part;            // splits > 1: [splits][N][M] partial products
@@ -116,7 +145,7 @@ template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, i
   if (e.Z) store_vec(static_cast<T*>(e.Z) + (int64_t)n * e.ldz + m, v);
   if (e.act != LINEAR_ACT_NONE) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = act_value(v[i], e.act);
+    for (int i = 0; i < V; ++i) v[i] = act_value<T>(v[i], e.act);
   }
   if (e.residual) {
     load_vec(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, x);
@@ -130,7 +159,7 @@ template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, i
 template <class T> __device__ inline void finish_one(const Epilogue& e, int m, int n, float v) {
   if (e.bias) v += (float)static_cast<const T*>(e.bias)[m];
   if (e.Z) static_cast<T*>(e.Z)[(int64_t)n * e.ldz + m] = (T)v;
-  v = act_value(v, e.act);
+  v = act_value<T>(v, e.act);
   if (e.residual) v += (float)static_cast<const T*>(e.residual)[(int64_t)n * e.ldr + m];
   static_cast<T*>(e.C)[(int64_t)n * e.ldc + m] = (T)v;
 }
@@ -138,7 +167,26 @@ template <class T> __device__ inline void finish_one(const Epilogue& e, int m, i
 // linear.hip.  Where A's (B's) contiguous index is the contraction, a_kc (b_kc)
 // is set; its rows are then ld apart, else its contraction indices are.
 int compute_units();
-int64_t product_workspace(int dtype, int64_t M, int64_t N, int64_t K);
+
+// An operand's lines (its contiguous extents): 16-byte aligned and whole 16 bytes
+// long, or not, or so far apart that a tile's offsets pass 32 bits.
+enum class Lines { kDirect, kRagged, kFar };
+
+inline Lines lines_of(int dtype, const void* p, int64_t ld, int64_t len) {
+  const int64_t size = dtype == LINEAR_F32 ? 4 : 2;
+  if (ld * size * 512 >= (1ll << 32) - 4096) return Lines::kFar;
+  return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && len * size % 16 == 0 ? Lines::kDirect : Lines::kRagged;
+}
+
+// The same before addresses are known.
+inline Lines lines_if(int dtype, bool aligned, int64_t len) {
+  return aligned && len * (dtype == LINEAR_F32 ? 4 : 2) % 16 == 0 ? Lines::kDirect : Lines::kRagged;
+}
+
+// Bytes of workspace for a product.
+int64_t product_workspace(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int64_t N, int64_t K);
+
+// p.arows, aK, brows, bK: the extents as loaded, or 0 where they are M, N and K.
 hipError_t launch_product(int dtype, bool a_kc, bool b_kc, Product p, void* workspace, hipStream_t s);
 
 // Argument checks of the C ABI.

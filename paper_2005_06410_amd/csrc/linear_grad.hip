@@ -10,14 +10,15 @@
 namespace linear {
 namespace {
 
-// dZ and the sums of its rows.  A workgroup owns 32 vectors (128 or 256 rows)
-// of `span` tokens; its eight groups of 32 lanes take every eighth token.  The
-// sums are of the fp32 values, before dZ is rounded.  Bound by memory: one
-// read of dO and Z and one write of dZ.
-template <class T, bool ACT, bool SUM>
+// dZ (WRITE: to lines of lddz values with zeros behind the last one; ACT: dO
+// times the slope at Z, else dO itself) and (SUM) the sums of its rows.  A
+// workgroup owns 32 vectors (128 or 256 rows) of `span` tokens; its eight groups
+// of 32 lanes take every eighth token.  The sums are of the fp32 values, before
+// dZ is rounded.  Bound by memory: one read of dO and Z and one write of dZ.
+template <class T, bool ACT, bool WRITE, bool SUM>
 __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, const T* __restrict__ dO, int64_t lddo,
-                                                    const T* __restrict__ Z, int64_t ldz, int act, T* __restrict__ dZ, int64_t lddz,
-                                                    float* __restrict__ part, T* __restrict__ dbias) {
+                                                    const T* __restrict__ Z, int64_t ldz, int act, T* __restrict__ dZ,
+                                                    int64_t lddz, float* __restrict__ part, T* __restrict__ dbias) {
   constexpr int V = kVec<T>;
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int m = (blockIdx.x * 32 + x) * V;
@@ -33,9 +34,9 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
       if (ACT) {
         load_vec(Z + (int64_t)n * ldz + m, z);
 #pragma unroll
-        for (int i = 0; i < V; ++i) d[i] = act_grad(d[i], z[i], act);
-        store_vec(dZ + (int64_t)n * lddz + m, d);
+        for (int i = 0; i < V; ++i) d[i] = act_grad<T>(d[i], z[i], act);
       }
+      if (WRITE) store_vec(dZ + (int64_t)n * lddz + m, d);
 #pragma unroll
       for (int i = 0; i < V; ++i) sum[i] += d[i];
     }
@@ -43,12 +44,12 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
     for (int n = lo + y; n < hi; n += 8) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (m + i >= kn) continue;
-        float d = (float)dO[(int64_t)n * lddo + m + i];
-        if (ACT) {
-          d = act_grad(d, (float)Z[(int64_t)n * ldz + m + i], act);
-          dZ[(int64_t)n * lddz + m + i] = (T)d;
+        float d = 0.0f;
+        if (m + i < kn) {
+          d = (float)dO[(int64_t)n * lddo + m + i];
+          if (ACT) d = act_grad<T>(d, (float)Z[(int64_t)n * ldz + m + i], act);
         }
+        if (WRITE && m + i < lddz) dZ[(int64_t)n * lddz + m + i] = (T)d;
         sum[i] += d;
       }
     }
@@ -71,11 +72,21 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
   }
 }
 
+// Adds the parts of dbias in a fixed order: 32 rows of a workgroup, eight groups
+// of lanes that take every eighth part.
 template <class T> __global__ __launch_bounds__(256) void bias_kernel(int kn, int parts, const float* part, T* dbias) {
-  const int k = blockIdx.x * 256 + threadIdx.x;
-  if (k >= kn) return;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, k = blockIdx.x * 32 + x;
+  __shared__ float sh[8][32];
   float s = 0.0f;
-  for (int i = 0; i < parts; ++i) s += part[(int64_t)i * kn + k];
+  if (k < kn) {
+#pragma unroll 8
+    for (int i = y; i < parts; i += 8) s += part[(int64_t)i * kn + k];
+  }
+  sh[y][x] = s;
+  __syncthreads();
+  if (y > 0 || k >= kn) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += sh[i][x];
   dbias[k] = (T)s;
 }
 
@@ -89,49 +100,66 @@ int slope_span(int dtype, int64_t kn, int64_t t) {
 
 // The workspace, in order.
 struct Layout {
-  int64_t lddz = 0;            // dZ (act only): kn rounded up to whole vectors
+  bool own = false;            // dZ is written here: an activation, or dO's lines are not direct
+  int64_t lddz = 0;            // kn rounded up to whole vectors
   int64_t part = 0;            // byte offset of the partial dbias
   int span = 0, parts = 0;
   int64_t product = 0;         // byte offset of the products' workspace
   int64_t bytes = 0;
 };
 
-Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act) {
+Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act, Lines f, Lines x, Lines d) {
   auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+  const int64_t vec = 16 / type_size(dtype);
   Layout w;
-  if (act != LINEAR_ACT_NONE) {
-    w.lddz = (kn + 7) / 8 * 8;
+  w.own = act != LINEAR_ACT_NONE || d == Lines::kFar || (d == Lines::kRagged && dtype != LINEAR_F32);
+  if (w.own) {
+    w.lddz = (kn + vec - 1) / vec * vec;
     w.part = up(w.lddz * t * type_size(dtype));
   }
+  if (w.own) d = Lines::kDirect;
   w.span = slope_span(dtype, kn, t);
   w.parts = (int)((t + w.span - 1) / w.span);
   w.product = w.part + (w.parts > 1 ? up((int64_t)w.parts * kn * 4) : 0);
-  w.bytes = w.product + std::max(product_workspace(dtype, ci, t, kn),
-                                 f_order ? product_workspace(dtype, ci, kn, t) : product_workspace(dtype, kn, ci, t));
+  w.bytes = w.product + std::max(product_workspace(dtype, f_order == 0, true, f, d, ci, t, kn),
+                                 f_order ? product_workspace(dtype, false, false, x, d, ci, kn, t)
+                                         : product_workspace(dtype, false, false, d, x, kn, ci, t));
   return w;
 }
 
 template <class T> hipError_t launch_slope(int64_t kn, int64_t t, const Layout& w, const void* dO, int64_t lddo, const void* Z,
                                            int64_t ldz, int act, char* ws, void* dbias, hipStream_t s) {
   const dim3 grid((unsigned)((kn + 32 * kVec<T> - 1) / (32 * kVec<T>)), (unsigned)std::max(1, w.parts));
-  auto k = act == LINEAR_ACT_NONE ? slope_kernel<T, false, true> : dbias ? slope_kernel<T, true, true> : slope_kernel<T, true, false>;
+  auto k = act != LINEAR_ACT_NONE ? (dbias ? slope_kernel<T, true, true, true> : slope_kernel<T, true, true, false>)
+           : w.own                ? (dbias ? slope_kernel<T, false, true, true> : slope_kernel<T, false, true, false>)
+                                  : slope_kernel<T, false, false, true>;
   float* part = w.parts > 1 ? reinterpret_cast<float*>(ws + w.part) : nullptr;
   k<<<grid, 256, 0, s>>>((int)kn, (int)t, w.span, static_cast<const T*>(dO), lddo, static_cast<const T*>(Z), ldz, act,
                          reinterpret_cast<T*>(ws), w.lddz, part, static_cast<T*>(dbias));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !dbias || !part) return e;
-  bias_kernel<T><<<dim3((unsigned)((kn + 255) / 256)), 256, 0, s>>>((int)kn, w.parts, part, static_cast<T*>(dbias));
+  bias_kernel<T><<<dim3((unsigned)((kn + 31) / 32)), 256, 0, s>>>((int)kn, w.parts, part, static_cast<T*>(dbias));
   return hipGetLastError();
 }
 
 }  // namespace
 }  // namespace linear
 
-extern "C" int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act) {
+extern "C" int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act,
+                                                     int aligned) {
   if (int e = linear::check_sizes(dtype, kn, ci, t)) return e;
   if (f_order != 0 && f_order != 1) return -5;
   if (act < LINEAR_ACT_NONE || act > LINEAR_ACT_SILU) return -6;
-  return linear::layout(dtype, kn, ci, t, f_order, act).bytes;
+  using namespace linear;
+  const Lines f = lines_if(dtype, aligned, f_order ? ci : kn), x = lines_if(dtype, aligned, ci), d = lines_if(dtype, aligned, kn);
+  const int64_t need = layout(dtype, kn, ci, t, f_order, act, f, x, d).bytes;
+  if (aligned) return need;
+  // any of the three may lie further apart than the direct loads reach
+  int64_t most = need;
+  for (int i = 1; i < 8; ++i)
+    most = std::max(most, layout(dtype, kn, ci, t, f_order, act, i & 1 ? Lines::kFar : f, i & 2 ? Lines::kFar : x,
+                                 i & 4 ? Lines::kFar : d).bytes);
+  return most;
 }
 
 extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order, int64_t ldf,
@@ -152,20 +180,23 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
   if (act != LINEAR_ACT_NONE && bad_ld(ldz, kn)) return -13;
   if (dX && bad_ld(lddx, ci)) return -16;
   if (dF && bad_ld(lddf, f_order ? ci : kn)) return -18;
-  const Layout w = layout(dtype, kn, ci, t, f_order, act);
+  const Layout w = layout(dtype, kn, ci, t, f_order, act, 
+                          dX ? lines_of(dtype, F, ldf, f_order ? ci : kn) : Lines::kDirect,
+                          dF ? lines_of(dtype, X, ldx, ci) : Lines::kDirect, lines_of(dtype, dO, lddo, kn));
   if (w.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return -20;
   if (workspace_bytes < w.bytes) return -21;
   char* ws = static_cast<char*>(workspace);
   hipError_t e = hipSuccess;
-  if (kn > 0 && (dbias || (act != LINEAR_ACT_NONE && t > 0))) {
+  if (kn > 0 && (dbias || (w.own && t > 0))) {
     switch (dtype) {
       case LINEAR_F32: e = launch_slope<float>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream); break;
       case LINEAR_BF16: e = launch_slope<bf16>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream); break;
       default: e = launch_slope<f16>(kn, t, w, dO, lddo, Z, ldz, act, ws, dbias, stream);
     }
   }
-  const void* dZ = act == LINEAR_ACT_NONE ? dO : workspace;
-  const int64_t lddz = act == LINEAR_ACT_NONE ? lddo : w.lddz;
+  const void* dZ = w.own ? workspace : dO;
+  const int64_t lddz = w.own ? w.lddz : lddo;
+  const int dz_rows = (int)(w.own ? w.lddz : kn);      // as loaded: zeros follow in the library's own copy
   if (e == hipSuccess && dX) {
     Product p{};
     p.A = F;
@@ -175,6 +206,7 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.M = (int)ci;
     p.N = (int)t;
     p.K = (int)kn;
+    p.bK = dz_rows;
     p.e.C = dX;
     p.e.ldc = lddx;
     e = launch_product(dtype, f_order == 0, true, p, ws + w.product, stream);
@@ -189,6 +221,7 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.M = (int)(f_order ? ci : kn);
     p.N = (int)(f_order ? kn : ci);
     p.K = (int)t;
+    (f_order ? p.brows : p.arows) = dz_rows;
     p.e.C = dF;
     p.e.ldc = lddf;
     e = launch_product(dtype, false, false, p, ws + w.product, stream);

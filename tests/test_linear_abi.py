@@ -63,11 +63,11 @@ def test_backward_argument_checks(lib, change, code):
 
 
 def test_workspace_queries(lib):
-    assert lib.convgemm_linear_workspace(F32, 0, 5, 5, 0) == 0
-    assert lib.convgemm_linear_workspace(9, 4, 4, 4, 0) == -1
-    assert lib.convgemm_linear_workspace(F32, 4, 4, 4, 2) == -5
-    assert lib.convgemm_linear_backward_workspace(F32, 4, 4, 4, 0, 5) == -6
-    assert lib.convgemm_linear_backward_workspace(BF16, 100, 50, 30, 1, 2) >= 100 * 30 * 2
+    assert lib.convgemm_linear_workspace(F32, 0, 5, 5, 0, 1) == 0
+    assert lib.convgemm_linear_workspace(9, 4, 4, 4, 0, 1) == -1
+    assert lib.convgemm_linear_workspace(F32, 4, 4, 4, 2, 1) == -5
+    assert lib.convgemm_linear_backward_workspace(F32, 4, 4, 4, 0, 5, 1) == -6
+    assert lib.convgemm_linear_backward_workspace(BF16, 100, 50, 30, 1, 2, 0) >= 100 * 30 * 2
     assert lib.convgemm_grad_workspace(-1) == -1
     assert 0 < lib.convgemm_grad_workspace(1) <= lib.convgemm_grad_workspace(1000)
 
