@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "linear.h"
 
 namespace linear {
@@ -70,40 +72,59 @@ template <class T> __device__ inline float tanh_gate(float z) {
   return inverse<T>(1.0f + exp_of<T>(-2.0f * u));
 }
 
-// act(z) in fp32.
-template <class T> __device__ inline float act_value(float z, int act) {
-  float e;
+// f(std::integral_constant) of the activation: one branch for a whole vector.
+template <class F> __device__ inline void with_act(int act, F f) {
   switch (act) {
-    case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-    case LINEAR_ACT_GELU: return z * normal_cdf<T>(z, e);
-    case LINEAR_ACT_GELU_TANH: return z * tanh_gate<T>(z);
-    case LINEAR_ACT_SILU: return z * inverse<T>(1.0f + exp_of<T>(-z));
-    default: return z;
+    case LINEAR_ACT_RELU: return f(std::integral_constant<int, LINEAR_ACT_RELU>{});
+    case LINEAR_ACT_GELU: return f(std::integral_constant<int, LINEAR_ACT_GELU>{});
+    case LINEAR_ACT_GELU_TANH: return f(std::integral_constant<int, LINEAR_ACT_GELU_TANH>{});
+    case LINEAR_ACT_SILU: return f(std::integral_constant<int, LINEAR_ACT_SILU>{});
   }
 }
 
+// act(z) in fp32.
+template <class T, int ACT> __device__ inline float act_value(float z) {
+  float e;
+  if constexpr (ACT == LINEAR_ACT_RELU) return z <= 0.0f ? 0.0f : z;
+  if constexpr (ACT == LINEAR_ACT_GELU) return z * normal_cdf<T>(z, e);
+  if constexpr (ACT == LINEAR_ACT_GELU_TANH) return z * tanh_gate<T>(z);
+  if constexpr (ACT == LINEAR_ACT_SILU) return z * inverse<T>(1.0f + exp_of<T>(-z));
+  return z;
+}
+
 // d act'(z) in fp32.
-template <class T> __device__ inline float act_grad(float d, float z, int act) {
-  switch (act) {
-    case LINEAR_ACT_RELU: return z <= 0.0f ? 0.0f : d;   // zero also where d is not finite
-    case LINEAR_ACT_GELU: {
-      float e;
-      const float c = normal_cdf<T>(z, e);
-      return d * (c + z * (0.3989422804014327f * e));
-    }
-    case LINEAR_ACT_GELU_TANH: {
-      // beyond 16 the slope is 0 or 1 to the last bit, and z^3 could overflow
-      if (z > 16.0f) return d;
-      if (z < -16.0f) return d * 0.0f;
-      const float s = tanh_gate<T>(z);
-      return d * (s + 2.0f * z * s * (1.0f - s) * kTanhScale * (1.0f + 3.0f * kTanhCubic * z * z));
-    }
-    case LINEAR_ACT_SILU: {
-      const float s = inverse<T>(1.0f + exp_of<T>(-z));
-      return d * (s * (1.0f + z * (1.0f - s)));
-    }
-    default: return d;
+template <class T, int ACT> __device__ inline float act_grad(float d, float z) {
+  if constexpr (ACT == LINEAR_ACT_RELU) return z <= 0.0f ? 0.0f : d;   // zero also where d is not finite
+  if constexpr (ACT == LINEAR_ACT_GELU) {
+    float e;
+    const float c = normal_cdf<T>(z, e);
+    return d * (c + z * (0.3989422804014327f * e));
   }
+  if constexpr (ACT == LINEAR_ACT_GELU_TANH) {
+    // beyond 16 the slope is 0 or 1 to the last bit, and z^3 could overflow
+    const float s = tanh_gate<T>(z);
+    const float slope = s + 2.0f * z * s * (1.0f - s) * kTanhScale * (1.0f + 3.0f * kTanhCubic * z * z);
+    return d * (z > 16.0f ? 1.0f : z < -16.0f ? 0.0f : slope);
+  }
+  if constexpr (ACT == LINEAR_ACT_SILU) {
+    const float s = inverse<T>(1.0f + exp_of<T>(-z));
+    return d * (s * (1.0f + z * (1.0f - s)));
+  }
+  return d;
+}
+
+template <class T, int N> __device__ inline void act_values(float* v, int act) {
+  with_act(act, [&](auto a) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<T, decltype(a)::value>(v[i]);
+  });
+}
+
+template <class T, int N> __device__ inline void act_grads(float* d, const float* z, int act) {
+  with_act(act, [&](auto a) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] = act_grad<T, decltype(a)::value>(d[i], z[i]);
+  });
 }
 
 // What follows a product: C = act(product + bias) + residual, Z = product + bias.
@@ -143,10 +164,7 @@ template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, i
     for (int i = 0; i < V; ++i) v[i] += x[i];
   }
   if (e.Z) store_vec(static_cast<T*>(e.Z) + (int64_t)n * e.ldz + m, v);
-  if (e.act != LINEAR_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = act_value<T>(v[i], e.act);
-  }
+  act_values<T, V>(v, e.act);
   if (e.residual) {
     load_vec(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, x);
 #pragma unroll
@@ -159,7 +177,7 @@ template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, i
 template <class T> __device__ inline void finish_one(const Epilogue& e, int m, int n, float v) {
   if (e.bias) v += (float)static_cast<const T*>(e.bias)[m];
   if (e.Z) static_cast<T*>(e.Z)[(int64_t)n * e.ldz + m] = (T)v;
-  v = act_value<T>(v, e.act);
+  act_values<T, 1>(&v, e.act);
   if (e.residual) v += (float)static_cast<const T*>(e.residual)[(int64_t)n * e.ldr + m];
   static_cast<T*>(e.C)[(int64_t)n * e.ldc + m] = (T)v;
 }

@@ -33,8 +33,7 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
       load_vec(dO + (int64_t)n * lddo + m, d);
       if (ACT) {
         load_vec(Z + (int64_t)n * ldz + m, z);
-#pragma unroll
-        for (int i = 0; i < V; ++i) d[i] = act_grad<T>(d[i], z[i], act);
+        act_grads<T, V>(d, z, act);
       }
       if (WRITE) store_vec(dZ + (int64_t)n * lddz + m, d);
 #pragma unroll
@@ -47,7 +46,10 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
         float d = 0.0f;
         if (m + i < kn) {
           d = (float)dO[(int64_t)n * lddo + m + i];
-          if (ACT) d = act_grad<T>(d, (float)Z[(int64_t)n * ldz + m + i], act);
+          if (ACT) {
+            const float z = (float)Z[(int64_t)n * ldz + m + i];
+            act_grads<T, 1>(&d, &z, act);
+          }
         }
         if (WRITE && m + i < lddz) dZ[(int64_t)n * lddz + m + i] = (T)d;
         sum[i] += d;
