@@ -513,10 +513,10 @@ struct Ring {
 template <class R> __global__ __launch_bounds__(R::NT, 2) void ring_kernel(Product p) { R::run(p); }
 
 // ---------------------------------------------------------------------------
-// the 256 x 256 product (both operands straight to LDS)
+// the 256 x 256 product (16-bit types, both operands straight to LDS)
 // ---------------------------------------------------------------------------
 // Eight waves, two by four, each with a 128 x 64 part of the tile. Per chunk a
-// wave's part is four quarters of 16 matrix instructions each (64 in fp32), and
+// wave's part is four quarters of 16 matrix instructions each, and
 // every quarter is a phase between two workgroup barriers:
 //   phase 0: rows half 0 x columns half 0    reads A0, B0
 //   phase 1: rows half 0 x columns half 1    reads B1
@@ -760,34 +760,47 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(Copy a, Cop
 // choice and launch
 // ---------------------------------------------------------------------------
 // The kernels: tile, chunks of a stage, stages, workgroups that a compute unit holds
-// (by their LDS), and what their time is made of (microseconds): `start` for a launch
-// and the first loads, `stage` the least time of a stage (its latencies), `rate`
-// the matrix cores' share that it reaches, `out` the result of a 64 x 64 part.
-// The figures are a fit to the times of 600 random products of layers with 64 ..
-// 16384 outputs and inputs and 1 .. 8192 tokens, every kernel with 1, 2, 4 and 8
-// splits, fp32 and bf16; over 4063 such products the choice by them is 1.7 %
-// slower on average than the fastest kernel of each.
-enum Shape { kWide, kSquare2, kSquare4, kTall, kSmall, kQuad64, kBlock32, kNarrow32, kNarrow16, kThin16, kRow80, kShapes };
-struct Tile {
-  int m, n, depth, stages, held;
+// (by their LDS), and, for fp32 and for the 16-bit types, what their time is made
+// of (microseconds): `start` for a launch and the first loads, `stage` the least
+// time of a stage (its latencies), `rate` the share of kRate that the matrix
+// instructions reach, `out` the result of a 64 x 64 part.
+// The figures are a fit to the times of 500 random products of layers with 64 ..
+// 16384 outputs and inputs and 1 .. 8192 tokens for each type, every kernel with
+// 1, 2, 4 and 8 splits; on 920 other such products the choice by them is 2.1 %
+// slower on average than the fastest kernel of each.  Without one of them the
+// fastest would be slower on average by (fp32 / bf16) 0 / 0.4 % (256 x 256), 0.3 /
+// 0.5 and 0 / 0.4 % (128 x 128), 0.2 / 0.1 % (128 x 64), 2.2 / 3.2 and 0.1 / 0.4 %
+// (64 x 64), 0.9 / 1.6 % (32 x 32), 0.1 / 0 % (64 x 32), 2.7 / 0.1 % (64 x 16),
+// 4.2 / 1.3 % (16 x 16), 0.1 / 0 % (32 x 80), 0.1 / 0 % (16 x 80); the large tiles matter where the work is large.
+enum Shape { kWide, kSquare2, kSquare4, kTall, kSmall, kQuad64, kBlock32, kNarrow32, kNarrow16, kThin16, kRow80, kSlim80, kShapes };
+struct Figures {
   float start, stage, rate, out;
 };
+struct Tile {
+  int m, n, depth, stages, held;
+  Figures f32, f16;
+};
 constexpr Tile kTiles[kShapes] = {
-    {256, 256, 1, 2, 1, 10.26f, 0.60f, 1.156f, 0.204f},  // eight waves in two groups that alternate
-    {128, 128, 1, 2, 2, 3.58f, 0.79f, 1.191f, 0.065f},   // two stages, two workgroups per unit
-    {128, 128, 1, 4, 1, 3.63f, 0.58f, 1.019f, 0.101f},   // four stages, eight waves
-    {128, 64, 1, 3, 2, 4.46f, 0.51f, 1.302f, 0.322f},
-    {64, 64, 1, 4, 2, 3.61f, 0.32f, 1.067f, 0.084f},
-    {64, 64, 2, 4, 1, 3.91f, 0.35f, 1.108f, 0.199f},     // eight waves, two per part of the tile
-    {32, 32, 4, 4, 1, 4.10f, 0.35f, 0.659f, 0.076f},     // four waves share the contraction
-    {64, 32, 4, 3, 1, 4.39f, 0.40f, 0.893f, 0.003f},
-    {64, 16, 4, 3, 1, 4.10f, 0.40f, 0.761f, 0.000f},
-    {16, 16, 8, 4, 1, 4.12f, 0.35f, 1.000f, 0.013f},     // eight waves share the contraction: one token's layer
-    {32, 80, 2, 2, 2, 4.60f, 1.10f, 1.000f, 0.001f}};    // fp32: a batch of 80 without a wasted column
-constexpr double kRate32 = 0.426e6, kRate16 = 6.30e6;   // operations per microsecond and compute unit
-constexpr double kLoadRate = 57.9e3;                    // bytes per microsecond into a compute unit's LDS
-constexpr double kReadRate = 6.28e6;                    // operands from memory
-constexpr double kJoin = 3.98, kJoinRate = 4.76e6;      // the launch that adds split contractions, and its bytes
+    {256, 256, 1, 2, 1,     {8.33f, 0.70f, 1.53f, 0.782f}, {4.90f, 0.60f, 1.02f, 0.181f}},  // eight waves in two groups that alternate (16-bit types)
+    {128, 128, 1, 2, 2,     {3.34f, 0.61f, 1.22f, 0.060f}, {3.49f, 0.87f, 1.18f, 0.073f}},  // two workgroups per unit
+    {128, 128, 1, 4, 1,     {2.87f, 0.44f, 1.25f, 0.187f}, {3.64f, 0.57f, 1.00f, 0.102f}},  // eight waves
+    {128, 64, 1, 3, 2,      {4.60f, 1.04f, 1.20f, 0.331f}, {4.08f, 0.45f, 1.06f, 0.199f}},
+    {64, 64, 1, 4, 2,       {3.85f, 0.26f, 1.07f, 0.097f}, {3.60f, 0.29f, 1.08f, 0.087f}},
+    {64, 64, 2, 4, 1,       {3.94f, 0.72f, 1.11f, 0.286f}, {4.06f, 0.36f, 0.85f, 0.043f}},  // eight waves, two for each part of the tile
+    {32, 32, 4, 4, 1,       {4.88f, 0.49f, 0.66f, 0.060f}, {4.10f, 0.31f, 1.01f, 0.065f}},  // four waves share the contraction
+    {64, 32, 4, 3, 1,       {4.21f, 0.33f, 0.89f, 0.012f}, {4.29f, 0.39f, 0.80f, 0.000f}},  // four waves share the contraction
+    {64, 16, 4, 3, 1,       {4.02f, 0.42f, 1.03f, 0.000f}, {4.02f, 0.44f, 0.78f, 0.000f}},  // four waves share the contraction
+    {16, 16, 8, 4, 1,       {4.37f, 0.40f, 1.22f, 0.003f}, {4.14f, 0.27f, 0.94f, 0.002f}},  // eight waves share the contraction: one token
+    {32, 80, 2, 2, 2,       {5.59f, 0.79f, 1.03f, 0.000f}, {5.59f, 0.82f, 1.10f, 0.001f}},  // fp32: a batch of 80 without a wasted column
+    {16, 80, 4, 3, 1,       {4.42f, 0.49f, 0.82f, 0.118f}, {4.42f, 0.49f, 0.82f, 0.118f}},  // the same, eight waves share the contraction
+};
+struct Rates {
+  double mul;             // operations per microsecond and compute unit
+  double load;            // bytes per microsecond into a compute unit's LDS
+  double read;            // bytes per microsecond from memory
+  double join, join_rate; // the launch that adds split contractions, and its bytes
+};
+constexpr Rates kRates32 = {0.4259e6, 51.7e3, 4.82e6, 3.23, 2.78e6}, kRates16 = {6.741e6, 69.6e3, 4.87e6, 3.39, 3.17e6};
 
 struct Plan {
   Shape shape;
@@ -799,23 +812,25 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 double time_of(const Tile& t, bool f32, int width, int64_t M, int64_t N, int64_t K, int64_t splits, int64_t cu) {
   const int size = f32 ? 4 : 2;
+  const Figures& f = f32 ? t.f32 : t.f16;
+  const Rates& r = f32 ? kRates32 : kRates16;
   const int64_t deep = 128 / size * t.depth, groups = ceil_div(M, t.m) * ceil_div(N, t.n) * splits;
   const double steps = (double)ceil_div(ceil_div(K, deep), splits);
-  const double load = (t.m + t.n) * 128.0 * t.depth / kLoadRate * (width == 4 ? 4.0 : 1.0);
-  const double mul = 2.0 * t.m * t.n * deep / ((f32 ? kRate32 : kRate16) * t.rate);
+  const double load = (t.m + t.n) * 128.0 * t.depth / r.load * (width == 4 ? 4.0 : 1.0);   // four times as many loads
+  const double mul = 2.0 * t.m * t.n * deep / (r.mul * f.rate);
   auto round = [&](int64_t c) {   // c workgroups per compute unit at once
-    return steps * std::max<double>(t.stage, c * std::max(load, mul)) + t.out * c * (t.m * t.n / 4096.0);
+    return steps * std::max<double>(f.stage, c * std::max(load, mul)) + f.out * c * (t.m * t.n / 4096.0);
   };
   const int64_t full = groups / (t.held * cu), rest = groups % (t.held * cu);
-  double us = full * round(t.held) + (rest ? round(ceil_div(rest, cu)) : 0.0);
+  const double work = full * round(t.held) + (rest ? round(ceil_div(rest, cu)) : 0.0);
   // what the workgroups have under way bounds the rate of reading: about 2 us for
   // a load from memory, half of that from the last-level cache
   const double bytes = (double)size * ((double)M * K + (double)K * N);
   const double way = std::min(groups, t.held * cu) * (double)(std::min<int64_t>(t.m, M) + std::min<int64_t>(t.n, N)) * 128.0 *
                      t.depth * (t.stages - 1);
-  const double read = bytes / std::min(kReadRate, way / (bytes > 32e6 ? 2.0 : 1.0));
-  us = std::max(us, read) + 0.05 * std::min(us, read) + t.start;
-  if (splits > 1) us += kJoin + splits * (double)M * N * 8.0 / kJoinRate;
+  const double read = bytes / std::min(r.read, way / (bytes > 32e6 ? 2.0 : 1.0));
+  double us = std::max(work, read) + 0.05 * std::min(work, read) + f.start;
+  if (splits > 1) us += r.join + splits * (double)M * N * 8.0 / r.join_rate;
   return us;
 }
 
@@ -823,8 +838,10 @@ Plan search_plan(bool f32, int width, bool a_kc, bool b_kc, int64_t M, int64_t N
   Plan best{kSquare2, 1, 0.0};
   for (int i = 0; i < kShapes; ++i) {
     const Tile& t = kTiles[i];
-    if (i >= kNarrow32 && (!b_kc || N > 256)) continue;
-    if ((i == kThin16 && !a_kc) || (i == kRow80 && !f32) || (i == kWide && width != 16)) continue;
+    // narrow tiles read the weights again for every column of tiles, from memory
+    // where they are cold: four times at most
+    if (i >= kNarrow32 && (!b_kc || N > 4 * t.n)) continue;
+    if ((i == kThin16 && !a_kc) || ((i == kRow80 || i == kSlim80) && !f32) || (i == kWide && f32)) continue;
     const int64_t stages = ceil_div(K, (f32 ? 32 : 64) * t.depth);
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (splits > 1 && (stages < 2 * splits || ceil_div(M, t.m) * ceil_div(N, t.n) * splits > 4 * cu)) break;
@@ -880,7 +897,7 @@ Route route_of(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int
   if (!copied.copy_a && !copied.copy_b) return copied;
   if (dtype == LINEAR_F32 && a != Lines::kFar && b != Lines::kFar) {
     const int64_t values = (copied.copy_a ? copy_values(dtype, a_kc, M, K) : 0) + (copied.copy_b ? copy_values(dtype, b_kc, N, K) : 0);
-    const double copy = 5.0 + 2.0 * 4.0 * values / kReadRate;
+    const double copy = 5.0 + 2.0 * 4.0 * values / kRates32.read;
     if (plan_of(dtype, 4, a_kc, b_kc, M, N, K).us < plan_of(dtype, 16, a_kc, b_kc, M, N, K).us + copy) return Route{4, false, false};
   }
   if (b_kc && N <= 64) return Route{0, false, false};
@@ -906,7 +923,7 @@ template <class T, bool AKC, bool BKC> hipError_t launch_wide(Product p, hipStre
 }
 
 template <class T, bool AKC, bool BKC, int W> hipError_t launch_shape(Shape shape, const Product& p, hipStream_t s) {
-  if constexpr (W == 16) {
+  if constexpr (sizeof(T) == 2) {
     if (shape == kWide) return launch_wide<T, AKC, BKC>(p, s);
   }
   if (shape == kSquare4) return launch_ring<Ring<T, AKC, BKC, 4, 2, 2, 4, 1, 1, 4, W>>(p, s);
@@ -918,6 +935,7 @@ template <class T, bool AKC, bool BKC, int W> hipError_t launch_shape(Shape shap
     if (shape == kNarrow32) return launch_ring<Ring<T, AKC, BKC, 4, 2, 1, 1, 4, 4, 3, W>>(p, s);
     if (shape == kNarrow16) return launch_ring<Ring<T, AKC, BKC, 4, 1, 1, 1, 4, 4, 3, W>>(p, s);
     if constexpr (sizeof(T) == 4) {
+      if (shape == kSlim80) return launch_ring<Ring<T, AKC, BKC, 1, 5, 1, 1, 8, 4, 3, W>>(p, s);
       if (shape == kRow80) return launch_ring<Ring<T, AKC, BKC, 2, 5, 1, 1, 4, 2, 2, W>>(p, s);
     }
   }

@@ -93,11 +93,12 @@ template <class T> __global__ __launch_bounds__(256) void bias_kernel(int kn, in
 }
 
 // Tokens of one workgroup of slope_kernel: about four workgroups for each
-// compute unit, 32 tokens at least, 256 parts at most.
+// compute unit, 256 parts at most; up to 128 tokens one part, which needs no
+// second launch (80 tokens of 1000 rows: 4 us instead of 3 and 2.3).
 int slope_span(int dtype, int64_t kn, int64_t t) {
   const int64_t width = 32 * 16 / type_size(dtype), cols = (kn + width - 1) / width;
   const int64_t parts = std::min<int64_t>(256, std::max<int64_t>(1, 4 * compute_units() / std::max<int64_t>(cols, 1)));
-  return (int)std::max<int64_t>(32, (t + parts - 1) / parts);
+  return (int)(t <= 128 ? std::max<int64_t>(t, 1) : std::max<int64_t>(32, (t + parts - 1) / parts));
 }
 
 // The workspace, in order.
