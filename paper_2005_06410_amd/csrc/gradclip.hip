@@ -27,6 +27,10 @@ namespace {
 constexpr int kList = 240;          // tensors of one launch: the list travels in the kernel's arguments
 constexpr int64_t kTensorLimit = 1ll << 37;   // values of one tensor: the chunks of a list are below 2^31
 constexpr int kParts = 2048;        // partial sums (workgroups of the first pass)
+// Above this the scaled values are stored past the caches: what of the gradients
+// is still in the last-level cache stays there for the second pass (200 bf16
+// tensors, 180 MB: 99 -> 90 us).
+constexpr int64_t kStream = 128ll << 20;
 constexpr int kMinChunk = 4096;     // bytes that a workgroup takes at a time: one vector per thread ..
 constexpr int kMaxChunk = 32768;    // .. to eight
 
@@ -94,7 +98,7 @@ template <class T> __device__ inline double squares(const T* g, int64_t n) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-template <class T> __device__ inline void scale(const T* g, T* out, int64_t n, float c) {
+template <bool STREAM, class T> __device__ inline void scale(const T* g, T* out, int64_t n, float c) {
   constexpr int V = kVec<T>;
   for_values<T>(
       n,
@@ -107,7 +111,7 @@ template <class T> __device__ inline void scale(const T* g, T* out, int64_t n, f
         for (int u = 0; u < C; ++u) {
 #pragma unroll
           for (int j = 0; j < V; ++j) v[u][j] *= c;
-          store_vec(out + (int64_t)(i + 256 * u) * V, v[u]);
+          result_vec<T, STREAM>(out + (int64_t)(i + 256 * u) * V, v[u]);
         }
       },
       [&](int i) { out[i] = (T)((float)g[i] * c); });
@@ -156,6 +160,7 @@ __global__ __launch_bounds__(256) void total_kernel(const double* part, int part
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, int parts, double max_norm, float* norm) {
   const double v = total_norm(part, parts);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
@@ -166,11 +171,11 @@ __global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, 
   for_chunks<true>(l, lo, hi, [&](int i, int64_t at, int64_t n) {
     if (c == 1.0f && l.out[i] == l.g[i]) return;
     if (l.dtype[i] == LINEAR_F32)
-      scale(static_cast<const float*>(l.g[i]) + at, static_cast<float*>(l.out[i]) + at, n, c);
+      scale<STREAM>(static_cast<const float*>(l.g[i]) + at, static_cast<float*>(l.out[i]) + at, n, c);
     else if (l.dtype[i] == LINEAR_BF16)
-      scale(static_cast<const bf16*>(l.g[i]) + at, static_cast<bf16*>(l.out[i]) + at, n, c);
+      scale<STREAM>(static_cast<const bf16*>(l.g[i]) + at, static_cast<bf16*>(l.out[i]) + at, n, c);
     else
-      scale(static_cast<const f16*>(l.g[i]) + at, static_cast<f16*>(l.out[i]) + at, n, c);
+      scale<STREAM>(static_cast<const f16*>(l.g[i]) + at, static_cast<f16*>(l.out[i]) + at, n, c);
   });
 }
 
@@ -192,11 +197,15 @@ int take(List& l, int chunk, int from, int count, const void* const* g, void* co
   return from;
 }
 
-// Bytes of a chunk: as large as leaves every one of the first pass's workgroups
-// a chunk.
-int chunk_of(int count, const int64_t* n, const int* dtype) {
+int64_t bytes_of(int count, const int64_t* n, const int* dtype) {
   int64_t bytes = 0;
   for (int i = 0; i < count; ++i) bytes += n[i] * type_size(dtype[i]);
+  return bytes;
+}
+
+// Bytes of a chunk: as large as leaves every one of the first pass's workgroups
+// a chunk.
+int chunk_of(int64_t bytes) {
   int chunk = kMinChunk;
   while (chunk < kMaxChunk && bytes / (2 * chunk) >= kParts) chunk *= 2;
   return chunk;
@@ -211,7 +220,8 @@ int run(int count, const void* const* g, void* const* out, const int64_t* n, con
   double* part = static_cast<double*>(workspace);
   int parts = 0;
   List l;
-  const int chunk = chunk_of(count, n, dtype);
+  const int64_t bytes = bytes_of(count, n, dtype);
+  const int chunk = chunk_of(bytes);
   for (int at = 0; at < count;) {
     at = take(l, chunk, at, count, g, out, n, dtype);
     if (l.count == 0) break;
@@ -223,7 +233,8 @@ int run(int count, const void* const* g, void* const* out, const int64_t* n, con
   for (int at = 0; e == hipSuccess && out && at < count;) {
     at = take(l, chunk, at, count, g, out, n, dtype);
     if (l.count == 0) break;
-    scale_kernel<<<dim3(workgroups(l)), 256, 0, s>>>(l, part, parts, max_norm, told ? nullptr : norm);
+    const auto k = bytes >= kStream ? scale_kernel<true> : scale_kernel<false>;
+    k<<<dim3(workgroups(l)), 256, 0, s>>>(l, part, parts, max_norm, told ? nullptr : norm);
     told = true;
     e = hipGetLastError();
   }

@@ -310,7 +310,7 @@ __device__ inline void tile_of(int t, int mtiles, int ntiles, int& tm, int& tn) 
 // COLS columns of ROWS sums, staged by this wave ROWS + 4 floats apart, to the
 // result: rows m0 .., columns n0, n0 + step, ...  Neighbouring lanes take
 // neighbouring 16-byte results of a column.
-template <class T, int ROWS, int COLS>
+template <class T, int ROWS, int COLS, bool STREAM>
 __device__ inline void write_columns(const Product& p, int split, int m0, int n0, int step, int lane, const float* st) {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -333,7 +333,7 @@ __device__ inline void write_columns(const Product& p, int split, int m0, int n0
 #pragma unroll
         for (int i = 0; i < V; i += 4) store_vec(d + i, v + i);
       } else {
-        finish_vec<T>(p.e, m, n, v);
+        finish_vec<T, STREAM>(p.e, m, n, v);
       }
     } else {
       for (int i = 0; m + i < p.M; ++i) {
@@ -352,7 +352,7 @@ __device__ inline void write_columns(const Product& p, int split, int m0, int n0
 // Block column by block column: (16 WM) x 16 sums, then 16-byte results with
 // neighbouring lanes next to each other along M.
 // VA and VB neighbouring rows (columns) lie in neighbouring blocks (fp32 MC).
-template <class T, int VA, int VB, int WM, int WN>
+template <class T, int VA, int VB, bool STREAM = false, int WM, int WN>
 __device__ inline void write_tile(const Product& p, int split, int m0, int n0, int lane, char* lds, f4 (&acc)[WM][WN]) {
   constexpr int S = 16 * WM + 4;               // floats from one column to the next
   float* st = reinterpret_cast<float*>(lds);
@@ -374,7 +374,7 @@ __device__ inline void write_tile(const Product& p, int split, int m0, int n0, i
 #pragma unroll
       for (int i = 0; i < WM; ++i) *reinterpret_cast<f4*>(st + l16 * S + 16 * i + 4 * q) = acc[i][j];
     }
-    write_columns<T, 16 * WM, 16>(p, split, m0, n0 + 16 * VB * (j / VB) + j % VB, VB, lane, st);
+    write_columns<T, 16 * WM, 16, STREAM>(p, split, m0, n0 + 16 * VB * (j / VB) + j % VB, VB, lane, st);
   }
 }
 
@@ -592,7 +592,7 @@ template <class T, bool KC, int SR> struct WideStage {
 
 constexpr int kWideBuffer = 65536;                 // one chunk of both operands
 
-template <class T, bool AKC, bool BKC>
+template <class T, bool AKC, bool BKC, bool STREAM>
 __global__ __launch_bounds__(512) void wide_kernel(Product p) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tiles = p.mtiles * p.ntiles;
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(512) void wide_kernel(Product p) {
   // the loads past the end wrote zeros; LDS is free after them
   wait_loads<0>();
   workgroup_barrier();
-  write_tile<T, neighbours<T, AKC>(4), neighbours<T, BKC>(2)>(p, split, tm * 256 + wm * 128, tn * 256 + wn * 64, lane,
+  write_tile<T, neighbours<T, AKC>(4), neighbours<T, BKC>(2), STREAM>(p, split, tm * 256 + wm * 128, tn * 256 + wn * 64, lane,
                                                               smem + wave * (16 * 8 + 4) * 16 * 4, acc);
 }
 
@@ -916,9 +916,13 @@ template <class R> hipError_t launch_ring(Product p, hipStream_t s) {
 template <class T, bool AKC, bool BKC> hipError_t launch_wide(Product p, hipStream_t s) {
   p.mtiles = (p.M + 255) / 256;
   p.ntiles = (p.N + 255) / 256;
-  const hipError_t e = ltlt::ensure_dynamic_lds((const void*)wide_kernel<T, AKC, BKC>, 2 * kWideBuffer);
+  // 4096 x 16384 by 8192 tokens and back, bf16: 1728 us with ordinary stores, 1710 past
+  // the caches; 2048 x 8192 by 2048 (33 MB in between): 137 and 141
+  const bool stream = (int64_t)p.M * p.N * (int)sizeof(T) >= (64ll << 20);
+  auto k = stream ? wide_kernel<T, AKC, BKC, true> : wide_kernel<T, AKC, BKC, false>;
+  const hipError_t e = ltlt::ensure_dynamic_lds((const void*)k, 2 * kWideBuffer);
   if (e != hipSuccess) return e;
-  wide_kernel<T, AKC, BKC><<<dim3((unsigned)((int64_t)p.mtiles * p.ntiles * p.splits)), 512, 2 * kWideBuffer, s>>>(p);
+  k<<<dim3((unsigned)((int64_t)p.mtiles * p.ntiles * p.splits)), 512, 2 * kWideBuffer, s>>>(p);
   return hipGetLastError();
 }
 

@@ -127,6 +127,20 @@ template <class T, int N> __device__ inline void act_grads(float* d, const float
   });
 }
 
+// store_vec(), past the caches with STREAM: for results so large that keeping them
+// only drives out what is still read.
+template <class T, bool STREAM> __device__ inline void result_vec(T* p, const float* v) {
+  if constexpr (STREAM) {
+    typedef uint32_t w4 __attribute__((ext_vector_type(4), aligned(2)));
+    Packed<T> q;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) q.v[i] = (T)v[i];
+    __builtin_nontemporal_store(__builtin_bit_cast(w4, q), reinterpret_cast<w4*>(p));
+  } else {
+    store_vec(p, v);
+  }
+}
+
 // What follows a product: C = act(product + bias) + residual, Z = product + bias.
 struct Epilogue {
   const void* bias;       // M values or nullptr
@@ -155,7 +169,7 @@ struct Product {
 
 // kVec values m .. of column n of the result (all of them inside it); v holds
 // the product's fp32 sums.
-template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, int n, float* v) {
+template <class T, bool STREAM = false> __device__ inline void finish_vec(const Epilogue& e, int m, int n, float* v) {
   constexpr int V = kVec<T>;
   float x[V];
   if (e.bias) {
@@ -163,14 +177,14 @@ template <class T> __device__ inline void finish_vec(const Epilogue& e, int m, i
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += x[i];
   }
-  if (e.Z) store_vec(static_cast<T*>(e.Z) + (int64_t)n * e.ldz + m, v);
+  if (e.Z) result_vec<T, STREAM>(static_cast<T*>(e.Z) + (int64_t)n * e.ldz + m, v);
   act_values<T, V>(v, e.act);
   if (e.residual) {
     load_vec(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, x);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += x[i];
   }
-  store_vec(static_cast<T*>(e.C) + (int64_t)n * e.ldc + m, v);
+  result_vec<T, STREAM>(static_cast<T*>(e.C) + (int64_t)n * e.ldc + m, v);
 }
 
 // The same for one value, where a whole vector would pass the last row.
