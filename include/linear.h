@@ -81,13 +81,15 @@ int64_t convgemm_linear_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, 
 
 /* The kernel that convgemm_linear takes for a layer on the current device (host
  * only; without a device, on one of 256 CUs; `aligned` as above).  HOST int
- * out[5]:
+ * out[6]:
  *   out[0] = 1 the 256 x 256 tile's kernel, 2 a kernel with another tile, 3 one
  *            that loads single fp32 values, 4 loads through registers; 0 where
  *            there is nothing to do;
  *   out[1], out[2] = its tile, outputs x tokens;
  *   out[3] = workgroups that share a tile's contraction (added in a fixed order);
- *   out[4] = operands that are copied first. */
+ *   out[4] = operands that are copied first;
+ *   out[5] = the kernel's number among those of family 1 to 3 (two kernels may
+ *            have the same tile). */
 int convgemm_linear_choice(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int aligned, int* out);
 
 /* O = act(F X + bias) + residual.

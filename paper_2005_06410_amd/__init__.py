@@ -47,6 +47,7 @@ __all__ = [
     "convgemm",
     "linear",
     "linear_backward",
+    "linear_choice",
     "grad_norm",
     "clip_grad_norm",
     "LtltError",
@@ -613,9 +614,9 @@ def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, k
 
 def linear_choice(dtype, kn: int, ci: int, t: int, f_order: int = 1, aligned: bool = True):
     """The kernel that ``linear`` takes for a layer, as (family, tile outputs,
-    tile tokens, splits, copies): see ``convgemm_linear_choice``.  Host only;
+    tile tokens, splits, copies, kernel): see ``convgemm_linear_choice``.  Host only;
     ``f_order`` 1 for row-major weights, 0 for the convolution's order."""
-    out = (ctypes.c_int * 5)()
+    out = (ctypes.c_int * 6)()
     _check("convgemm_linear_choice", load().convgemm_linear_choice(
         _layer_dtype(dtype), int(kn), int(ci), int(t), int(f_order), int(bool(aligned)), ctypes.addressof(out)))
     return tuple(out)

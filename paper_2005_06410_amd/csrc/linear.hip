@@ -1016,17 +1016,17 @@ template <class T> hipError_t launch_typed(int dtype, bool a_kc, bool b_kc, Prod
 
 void product_choice(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int64_t N, int64_t K, int* out) {
   if (M <= 0 || N <= 0) {
-    for (int i = 0; i < 5; ++i) out[i] = 0;
+    for (int i = 0; i < 6; ++i) out[i] = 0;
     return;
   }
   const Route r = route_of(dtype, a_kc, b_kc, a, b, M, N, K);
   if (r.width == 0) {
-    out[0] = 4, out[1] = 64, out[2] = N <= 16 ? 16 : 64, out[3] = register_splits(dtype, M, N, K), out[4] = 0;
+    out[0] = 4, out[1] = 64, out[2] = N <= 16 ? 16 : 64, out[3] = register_splits(dtype, M, N, K), out[4] = 0, out[5] = 0;
   } else {
     const Plan p = plan_of(dtype, r.width, a_kc, b_kc, M, N, K);
     const Tile& t = kTiles[p.shape];
     out[0] = p.shape == kWide ? 1 : r.width == 16 ? 2 : 3;
-    out[1] = t.m, out[2] = t.n, out[3] = p.splits, out[4] = r.copy_a + r.copy_b;
+    out[1] = t.m, out[2] = t.n, out[3] = p.splits, out[4] = r.copy_a + r.copy_b, out[5] = p.shape;
   }
 }
 
