@@ -320,27 +320,29 @@ __device__ inline void write_columns(const Product& p, int split, int m0, int n0
     const int col = x / PER, row = (x % PER) * V;
     const int n = n0 + step * col, m = m0 + row;
     const float* src = st + col * (ROWS + 4) + row;
-    if (n >= p.N) continue;
-    if (m + V <= p.M) {
-      float v[V];
+    if (n >= p.N || m >= p.M) continue;
+    const int cnt = min(V, p.M - m);
+    auto sums = [&](float* v) {
 #pragma unroll
       for (int i = 0; i < V; i += 4) {
         const f4 w = *reinterpret_cast<const f4*>(src + i);
         v[i] = w[0], v[i + 1] = w[1], v[i + 2] = w[2], v[i + 3] = w[3];
       }
-      if (p.splits > 1) {
-        float* d = p.part + ((int64_t)split * p.N + n) * p.M + m;
+    };
+    if (p.splits == 1) {
+      if (cnt == V)
+        finish<T, true, STREAM>(p.e, m, n, cnt, sums);
+      else
+        finish<T, false, STREAM>(p.e, m, n, cnt, sums);
+    } else {
+      float* d = p.part + ((int64_t)split * p.N + n) * p.M + m;
+      if (cnt == V) {
+        float v[V];
+        sums(v);
 #pragma unroll
         for (int i = 0; i < V; i += 4) store_vec(d + i, v + i);
       } else {
-        finish_vec<T, STREAM>(p.e, m, n, v);
-      }
-    } else {
-      for (int i = 0; m + i < p.M; ++i) {
-        if (p.splits > 1)
-          p.part[((int64_t)split * p.N + n) * p.M + m + i] = src[i];
-        else
-          finish_one<T>(p.e, m + i, n, src[i]);
+        for (int i = 0; i < cnt; ++i) d[i] = src[i];
       }
     }
   }
@@ -687,34 +689,36 @@ __global__ __launch_bounds__(512) void wide_kernel(Product p) {
                                                               smem + wave * (16 * 8 + 4) * 16 * 4, acc);
 }
 
-// Sums the partial products of a split contraction in order and finishes them.
+// Sums the partial products of a split contraction in order and finishes them:
+// first every whole vector, then value by value what the columns have left over,
+// so that a wave has one kind only.
 template <class T> __global__ __launch_bounds__(256) void join_kernel(Product p) {
   constexpr int V = kVec<T>;
-  const int per = (p.M + V - 1) / V;
-  const int64_t total = (int64_t)per * p.N;
+  const int per = p.M / V, rest = p.M - per * V;
+  const int64_t whole = (int64_t)per * p.N, total = whole + (int64_t)rest * p.N, next = (int64_t)p.N * p.M;
   for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (int64_t)gridDim.x * 256) {
-    const int n = (int)(x / per), m = (int)(x - (int64_t)n * per) * V;
-    const float* d = p.part + (int64_t)n * p.M + m;
-    const int64_t next = (int64_t)p.N * p.M;
-    if (m + V <= p.M) {
-      float v[V], w[4];
+    if (x < whole) {
+      const int n = (int)(x / per), m = (int)(x - (int64_t)n * per) * V;
+      const float* d = p.part + (int64_t)n * p.M + m;
+      finish<T, true, false>(p.e, m, n, V, [&](float* v) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = 0.0f;
-      for (int s = 0; s < p.splits; ++s, d += next) {
+        for (int i = 0; i < V; ++i) v[i] = 0.0f;
+        for (int s = 0; s < p.splits; ++s, d += next) {
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-          load_vec(d + i, w);
+          for (int i = 0; i < V; i += 4) {
+            float w[4];
+            load_vec(d + i, w);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[i + j] += w[j];
+            for (int j = 0; j < 4; ++j) v[i + j] += w[j];
+          }
         }
-      }
-      finish_vec<T>(p.e, m, n, v);
+      });
     } else {
-      for (int i = 0; m + i < p.M; ++i) {
-        float v = 0.0f;
-        for (int s = 0; s < p.splits; ++s) v += d[s * next + i];
-        finish_one<T>(p.e, m + i, n, v);
-      }
+      const int n = (int)((x - whole) / rest), m = per * V + (int)((x - whole) % rest);
+      const float* d = p.part + (int64_t)n * p.M + m;
+      float v = 0.0f;
+      for (int s = 0; s < p.splits; ++s) v += d[s * next];
+      finish_one<T>(p.e, m, n, v);
     }
   }
 }
@@ -1007,7 +1011,7 @@ template <class T> hipError_t launch_typed(int dtype, bool a_kc, bool b_kc, Prod
     }
   }
   if (e != hipSuccess || p.splits == 1) return e;
-  const int64_t vecs = (int64_t)((p.M + kVec<T> - 1) / kVec<T>) * p.N;
+  const int64_t vecs = (p.M / kVec<T> + p.M % kVec<T>) * (int64_t)p.N;
   join_kernel<T><<<dim3((unsigned)std::min<int64_t>((vecs + 255) / 256, 4096)), 256, 0, s>>>(p);
   return hipGetLastError();
 }
