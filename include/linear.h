@@ -135,7 +135,7 @@ int convgemm_grad_norm(int count, const void* const* g, const int64_t* n, const 
 
 /* The same, and out[i] = c g[i] with c = min(1, max_norm / norm); out[i] has
  * g[i]'s type and order and may be g[i] itself (then nothing is written where
- * c = 1).  max_norm >= 0. */
+ * c = 1); the out[i] may not overlap one another.  max_norm >= 0. */
 int convgemm_grad_clip(int count, const void* const* g, void* const* out, const int64_t* n, const int* dtype,
                        double max_norm, float* norm, void* workspace, int64_t workspace_bytes, hipStream_t stream);
 

@@ -707,7 +707,8 @@ def clip_grad_norm(grads, max_norm: float, out=None):
     sizes, types and order in memory).  Returns the norm before scaling, as
     ``grad_norm`` does; nothing is copied to the host.
 
-    An infinite norm makes c zero and a NaN norm makes it NaN."""
+    An infinite norm makes c zero and a NaN norm makes it NaN.  The tensors to be
+    scaled may not overlap one another (the same one twice is refused)."""
     if not max_norm >= 0:
         raise ValueError("max_norm must be at least 0")
     return _norm_and_clip(grads, float(max_norm), out)
@@ -722,6 +723,9 @@ def _norm_and_clip(grads, max_norm, out):
                 [o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))
                  for o, g in zip(outs, grads)])):
             raise ValueError("out must have the gradients' sizes, types, order in memory and GPU")
+    if max_norm is not None and len(set(optrs)) != len(optrs) and len(
+            {p for p, n in zip(optrs, sizes) if n}) != len(sizes) - sizes.count(0):
+        raise ValueError("a tensor to be scaled is named twice")
     norm = grads[0].new_empty((), dtype=_torch().float32)
     count = len(grads)
     need = _scratch_bytes("convgemm_grad_workspace", dev, count)

@@ -1070,10 +1070,12 @@ extern "C" int64_t convgemm_linear_workspace(int dtype, int64_t kn, int64_t ci, 
   using namespace linear;
   if (int e = check_sizes(dtype, kn, ci, t)) return e;
   if (f_order != 0 && f_order != 1) return -5;
-  const Lines f = lines_if(dtype, aligned, f_order ? ci : kn), x = lines_if(dtype, aligned, ci);
-  const int64_t need = product_workspace(dtype, f_order == 1, true, f, x, kn, t, ci);
-  // lines further apart than the direct loads reach are copied or loaded through registers
-  return aligned ? need : std::max(need, product_workspace(dtype, f_order == 1, true, Lines::kFar, Lines::kFar, kn, t, ci));
+  if (aligned)
+    return product_workspace(dtype, f_order == 1, true, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci), kn, t, ci);
+  int64_t most = 0;
+  for (Lines f : kAnyLines)
+    for (Lines x : kAnyLines) most = std::max(most, product_workspace(dtype, f_order == 1, true, f, x, kn, t, ci));
+  return most;
 }
 
 extern "C" int convgemm_linear_choice(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int aligned, int* out) {

@@ -228,6 +228,7 @@ int compute_units();
 // An operand's lines (its contiguous extents): 16-byte aligned and whole 16 bytes
 // long, or not, or so far apart that a tile's offsets pass 32 bits.
 enum class Lines { kDirect, kRagged, kFar };
+constexpr Lines kAnyLines[] = {Lines::kDirect, Lines::kRagged, Lines::kFar};
 
 inline Lines lines_of(int dtype, const void* p, int64_t ld, int64_t len) {
   const int64_t size = dtype == LINEAR_F32 ? 4 : 2;

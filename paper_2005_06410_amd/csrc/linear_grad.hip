@@ -154,14 +154,13 @@ extern "C" int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int
   if (f_order != 0 && f_order != 1) return -5;
   if (act < LINEAR_ACT_NONE || act > LINEAR_ACT_SILU) return -6;
   using namespace linear;
-  const Lines f = lines_if(dtype, aligned, f_order ? ci : kn), x = lines_if(dtype, aligned, ci), d = lines_if(dtype, aligned, kn);
-  const int64_t need = layout(dtype, kn, ci, t, f_order, act, f, x, d).bytes;
-  if (aligned) return need;
-  // any of the three may lie further apart than the direct loads reach
-  int64_t most = need;
-  for (int i = 1; i < 8; ++i)
-    most = std::max(most, layout(dtype, kn, ci, t, f_order, act, i & 1 ? Lines::kFar : f, i & 2 ? Lines::kFar : x,
-                                 i & 4 ? Lines::kFar : d).bytes);
+  if (aligned)
+    return layout(dtype, kn, ci, t, f_order, act, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci),
+                  lines_if(dtype, true, kn)).bytes;
+  int64_t most = 0;
+  for (Lines f : kAnyLines)
+    for (Lines x : kAnyLines)
+      for (Lines d : kAnyLines) most = std::max(most, layout(dtype, kn, ci, t, f_order, act, f, x, d).bytes);
   return most;
 }
 

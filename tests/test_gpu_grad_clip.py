@@ -112,3 +112,15 @@ def test_not_finite(bad):
 def test_reproducible():
     grads = some([333_333, 1, 70_001], ["float32", "float16"])
     assert len({float(lt().grad_norm(grads)) for _ in range(5)}) == 1
+
+
+def test_the_same_tensor_twice():
+    """Counted twice in a norm; refused where it would be scaled twice at once."""
+    g = torch.full((8,), 2.0, device="cuda")
+    e = torch.zeros(0, device="cuda")
+    assert float(lt().grad_norm([g, g])) == 8.0
+    with pytest.raises(ValueError):
+        lt().clip_grad_norm([g, e, e, g], 1.0)
+    out = [torch.empty_like(g), e, e, torch.empty_like(g)]
+    assert float(lt().clip_grad_norm([g, e, e, g], 4.0, out=out)) == 8.0
+    assert (out[0] == 1.0).all() and (out[3] == 1.0).all() and (g == 2.0).all()

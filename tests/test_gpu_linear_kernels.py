@@ -117,6 +117,23 @@ def test_lines_far_apart(dtype, order, t):
     same(dF, dO.double() @ X.double().t(), "dF")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [2, 700])
+def test_long_aligned_lines(dtype, t):
+    """Lines far apart but aligned, near the limit of the direct loads on both
+    sides: the workspace that is asked for holds what the call takes."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    for ld in ((1 << 20) + 64, (1 << 21) - 64, (1 << 21) + 64):
+        F = torch.zeros(ld * 184, dtype=dtype, device="cuda").as_strided((184, 2760), (ld, 1))
+        F.copy_(ints(g, (184, 2760), 0.01, torch.float32))
+        X, dO = ints(g, (2760, t), 1.0, dtype), ints(g, (184, t), 0.1, dtype)
+        same(lt().linear(F, X), F.double() @ X.double(), "O")
+        dX, dF, _ = lt().linear_backward(F, X, dO)
+        same(dX, F.double().t() @ dO.double(), "dX")
+        same(dF, dO.double() @ X.double().t(), "dF")
+
+
 @pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("t", [3, 520])
 def test_weights_above_four_gib(order, t):

@@ -72,6 +72,17 @@ def test_workspace_queries(lib):
     assert 0 < lib.convgemm_grad_workspace(1) <= lib.convgemm_grad_workspace(1000)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_workspace_without_alignment_is_enough_for_any(lib, dtype):
+    """aligned = 0 covers every alignment that the sizes allow."""
+    for kn, ci, t in [(64, 4096, 5), (1000, 4096, 300), (24, 2456, 7), (1536, 1024, 2048), (184, 2760, 2), (33, 70001, 64)]:
+        for order in (0, 1):
+            assert lib.convgemm_linear_workspace(dtype, kn, ci, t, order, 0) >= lib.convgemm_linear_workspace(dtype, kn, ci, t, order, 1)
+            for act in (0, 2):
+                assert (lib.convgemm_linear_backward_workspace(dtype, kn, ci, t, order, act, 0)
+                        >= lib.convgemm_linear_backward_workspace(dtype, kn, ci, t, order, act, 1))
+
+
 def arrays(n=(4, 4), dtype=(F32, BF16), ptr=(16, 32)):
     return ((ctypes.c_void_p * 2)(*ptr), (ctypes.c_int64 * 2)(*n), (ctypes.c_int * 2)(*dtype))
 
