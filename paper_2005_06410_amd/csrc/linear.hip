@@ -400,7 +400,10 @@ template <class T> __device__ inline Operand<T> operand_b(const Product& p) {
 // of DEPTH chunks whose 2 DEPTH fragment groups are shared by WAVES_K groups of
 // waves; the groups' sums are added in order at the end.  LDS is a ring of
 // STAGES stages: the loads of stage s + STAGES - 1 are issued before stage s is
-// multiplied, so STAGES - 1 stages are under way at any time.
+// multiplied, so STAGES - 1 stages are under way at any time.  For few tokens the
+// bound is the bytes under way: 16384 x 4096 bf16 weights by 8 tokens run at 5.6 TB/s
+// with 73 KB per compute unit, at 3.5 with 27; for tens to hundreds of tokens it is
+// what the L2 caches deliver (about 12 TB/s) and a stage's own latencies (0.3 us).
 template <class T, bool AKC, bool BKC, int WM, int WN, int WAVES_M, int WAVES_N, int WAVES_K, int DEPTH, int STAGES, int WIDTH>
 struct Ring {
   static constexpr bool DMA = WIDTH > 0;
@@ -531,6 +534,10 @@ template <class R> __global__ __launch_bounds__(R::NT, 2) void ring_kernel(Produ
 // phase) always means: what the next phase reads is there, and every load has
 // four phases to arrive. The upper four waves run one barrier behind the
 // lower four, so that on every SIMD one wave reads while the other multiplies.
+// 8192^3 bf16: 1406 TFLOP/s with the contraction contiguous in both operands, 1350
+// and 1332 with one and none, 5 % less on a slower card (library product: 1411, 1227,
+// 1086; the 128 x 128 ring: 1050 at 4096^3).  Bound by the matrix cores at the clock that they hold; between
+// tiles, by the results, which are written while no product runs.
 // One operand of the wide product: sub-tiles of SR rows (64 of A, 32 of B) x
 // 128 bytes, each as in Stage. Half h of the operand is the sub-tiles 2 s + h.
 template <class T, bool KC, int SR> struct WideStage {
@@ -770,12 +777,14 @@ template <class T> __global__ __launch_bounds__(256) void pad_kernel(Copy a, Cop
 // instructions reach, `out` the result of a 64 x 64 part.
 // The figures are a fit to the times of 500 random products of layers with 64 ..
 // 16384 outputs and inputs and 1 .. 8192 tokens for each type, every kernel with
-// 1, 2, 4 and 8 splits; on 920 other such products the choice by them is 2.1 %
-// slower on average than the fastest kernel of each.  Without one of them the
-// fastest would be slower on average by (fp32 / bf16) 0 / 0.4 % (256 x 256), 0.3 /
-// 0.5 and 0 / 0.4 % (128 x 128), 0.2 / 0.1 % (128 x 64), 2.2 / 3.2 and 0.1 / 0.4 %
-// (64 x 64), 0.9 / 1.6 % (32 x 32), 0.1 / 0 % (64 x 32), 2.7 / 0.1 % (64 x 16),
-// 4.2 / 1.3 % (16 x 16), 0.1 / 0 % (32 x 80), 0.1 / 0 % (16 x 80); the large tiles matter where the work is large.
+// 1, 2, 4 and 8 splits, operands in the caches.  On 741 (fp32) and 179 (bf16)
+// other such products the choice by them is 3.1 and 1.7 % slower on average than
+// the fastest kernel of each.  Without one of the kernels the fastest would be
+// slower on average by (fp32 / bf16) 0.4 % for bf16 (256 x 256), 0.3 / 0.5 and 0 /
+// 0.4 % (128 x 128), 0.2 / 0.1 % (128 x 64), 2.2 / 3.2 and 0.1 / 0.4 % (64 x 64),
+// 0.9 / 1.6 % (32 x 32), 0.1 / 0 % (64 x 32), 2.7 / 0.1 % (64 x 16),
+// 4.2 / 1.3 % (16 x 16), 0.1 % for fp32 (32 x 80 and 16 x 80, which save about a
+// quarter at 80 tokens); the large tiles matter where the work is large.
 enum Shape { kWide, kSquare2, kSquare4, kTall, kSmall, kQuad64, kBlock32, kNarrow32, kNarrow16, kThin16, kRow80, kSlim80, kShapes };
 struct Figures {
   float start, stage, rate, out;
