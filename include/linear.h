@@ -26,9 +26,13 @@
  * Types: LINEAR_F32, LINEAR_BF16, LINEAR_F16; all tensors of one layer have the
  * same type.  Products are summed in fp32 on the matrix cores and the epilogue
  * is computed in fp32; each result is rounded to the type once.  Between the
- * two products of the gradients dZ is held in the layer's type (dbias is summed
- * from the values before that rounding).  norm is summed in fp64.  Every result
- * is reproducible: no sum depends on the order in which workgroups run.
+ * two products of the gradients dZ is held in the layer's type, one more rounding
+ * (exact for relu and without an activation): a 16-bit dX or dF is then off by
+ * about 1.4 roundings in its norm instead of one.  fp16 holds dZ times a power of
+ * two that is taken from the largest finite |dO|, so that no dZ overflows and
+ * small ones keep their digits.  dbias is summed from the values before that
+ * rounding.  norm is summed in fp64.  Every result is reproducible: no sum
+ * depends on the order in which workgroups run.
  *
  * Storage: X, O, residual, Z, dO and dX have their first index fastest and a
  * leading dimension (elements from one token to the next) of at least their

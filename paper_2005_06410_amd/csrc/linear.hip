@@ -1125,7 +1125,7 @@ extern "C" int convgemm_linear(int dtype, int64_t kn, int64_t ci, int64_t t, con
   p.M = (int)kn;
   p.N = (int)t;
   p.K = (int)ci;
-  p.e = linear::Epilogue{bias, residual, ldr, Z, ldz, O, ldo, act};
+  p.e = linear::Epilogue{bias, residual, ldr, Z, ldz, O, ldo, act, nullptr};
   const hipError_t e = linear::launch_product(dtype, f_order == 1, true, p, workspace, stream);
   return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
 }

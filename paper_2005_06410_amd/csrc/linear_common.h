@@ -141,7 +141,8 @@ template <class T, bool STREAM> __device__ inline void result_vec(T* p, const fl
   }
 }
 
-// What follows a product: C = act(product + bias) + residual, Z = product + bias.
+// What follows a product: C = act(product scale + bias) + residual, Z = product
+// scale + bias.
 struct Epilogue {
   const void* bias;       // M values or nullptr
   const void* residual;   // M x N or nullptr
@@ -151,6 +152,7 @@ struct Epilogue {
   void* C;
   int64_t ldc;
   int act;
+  const float* scale;     // fp16 only: one value (a power of two) or nullptr
 };
 
 // C (M x N, M fastest) = A (M x K) B (K x N).
@@ -199,6 +201,13 @@ __device__ inline void finish(const Epilogue& e, int m, int n, int cnt, F sums) 
   if (e.bias) load_part<T, WHOLE>(static_cast<const T*>(e.bias) + m, cnt, b);
   if (e.residual) load_part<T, WHOLE>(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, cnt, r);
   sums(v);
+  if constexpr (std::is_same_v<T, f16>) {
+    if (e.scale) {
+      const float c = *e.scale;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= c;
+    }
+  }
   if (e.bias) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += b[i];
@@ -214,6 +223,7 @@ __device__ inline void finish(const Epilogue& e, int m, int n, int cnt, F sums) 
 
 // The same for one value.
 template <class T> __device__ inline void finish_one(const Epilogue& e, int m, int n, float v) {
+  if (std::is_same_v<T, f16> && e.scale) v *= *e.scale;
   if (e.bias) v += (float)static_cast<const T*>(e.bias)[m];
   if (e.Z) static_cast<T*>(e.Z)[(int64_t)n * e.ldz + m] = (T)v;
   act_values<T, 1>(&v, e.act);

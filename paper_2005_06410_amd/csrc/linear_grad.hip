@@ -4,24 +4,103 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear_common.h"
 
 namespace linear {
 namespace {
 
+// dZ between the two products is held in the layer's type: one rounding, as large
+// as a result's own, so that a 16-bit dX or dF is off by about 1.4 roundings instead
+// of one (777 tokens through 1001 x 515, GELU, fp16: 2.9e-4 of its norm instead of
+// 2.1e-4; bf16: 2.3e-3 instead of 1.7e-3).  The matrix cores take both operands in
+// one type, and what the rounding leaves over would have to be multiplied as well,
+// twice the work.  relu's dZ is exact.
+//
+// fp16's range does not hold every dZ: GELU's slope reaches 1.13, so a dO from 57967
+// on gives an infinite one, and a small dO times a small slope lies below the
+// smallest value.  dZ is therefore held times a power of two that puts the largest
+// finite |dO| between 2^14 and 2^15 (the products' sums are multiplied back in
+// fp32): nothing finite overflows, and the lower end's spacing loses at most 2^-39
+// of the largest |dO|.
+constexpr int kPeaks = 512;
+
+__device__ inline float wave_max(float v) {
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// The largest finite |dO| of each workgroup's part, the parts as in slope_kernel.
+// One more read of dO (8192 tokens of 4096 rows: 67 MB).
+__global__ __launch_bounds__(256) void peak_kernel(int kn, int t, int span, int cols, int parts, const f16* __restrict__ dO,
+                                                   int64_t lddo, float* __restrict__ peaks) {
+  constexpr int V = kVec<f16>;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  float top = 0.0f;
+  auto take = [&](float d) {
+    d = fabsf(d);
+    top = fmaxf(top, d < INFINITY ? d : 0.0f);      // neither infinities nor NaN
+  };
+  for (int64_t at = blockIdx.x; at < (int64_t)cols * parts; at += gridDim.x) {
+    const int part = (int)(at / cols), m = ((int)(at - (int64_t)part * cols) * 32 + x) * V;
+    const int lo = part * span, hi = min(t, lo + span);
+    if (m + V <= kn) {
+#pragma unroll 4
+      for (int n = lo + y; n < hi; n += 8) {
+        float d[V];
+        load_vec(dO + (int64_t)n * lddo + m, d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) take(d[i]);
+      }
+    } else {
+      for (int n = lo + y; n < hi; n += 8)
+        for (int i = m; i < kn; ++i) take((float)dO[(int64_t)n * lddo + i]);
+    }
+  }
+  __shared__ float sh[4];
+  top = wave_max(top);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) peaks[blockIdx.x] = fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
+// The power of two by which dZ is held, the same in every wave: each reads all
+// peaks, so that no barrier stands between this and the loads that follow.
+__device__ inline float scale_of(const float* peaks, int count) {
+  float top = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kPeaks / 64; ++k) {
+    const int i = k * 64 + (int)(threadIdx.x & 63);
+    top = fmaxf(top, peaks[min(i, count - 1)]);
+  }
+  top = wave_max(top);
+  int e = 15;
+  if (top > 0.0f) frexpf(top, &e);                  // top in [2^(e-1), 2^e)
+  return ldexpf(1.0f, 15 - e);
+}
+
 // dZ (WRITE: to lines of lddz values with zeros behind the last one; ACT: dO
 // times the slope at Z, else dO itself) and (SUM) the sums of its rows.  A
 // workgroup owns 32 vectors (128 or 256 rows) of `span` tokens; its eight groups
 // of 32 lanes take every eighth token.  The sums are of the fp32 values, before
-// dZ is rounded.  Bound by memory: one read of dO and Z and
+// dZ is rounded.  With `peaks` (fp16) dZ is written times scale_of() and 1 /
+// scale_of() to `back`.  Bound by memory: one read of dO and Z and
 // one write of dZ (4096 rows, 8192 tokens, bf16: 15 us for dbias alone, 4.5 TB/s; 32
 // with GELU, 6 TB/s).
 template <class T, bool ACT, bool WRITE, bool SUM>
 __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, const T* __restrict__ dO, int64_t lddo,
                                                     const T* __restrict__ Z, int64_t ldz, int act, T* __restrict__ dZ,
-                                                    int64_t lddz, float* __restrict__ part, T* __restrict__ dbias) {
+                                                    int64_t lddz, float* __restrict__ part, T* __restrict__ dbias,
+                                                    const float* __restrict__ peaks, int npeaks, float* __restrict__ back) {
   constexpr int V = kVec<T>;
+  float scale = 1.0f;
+  if constexpr (ACT && WRITE && std::is_same_v<T, f16>) {
+    if (peaks) {
+      scale = scale_of(peaks, npeaks);
+      if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *back = 1.0f / scale;
+    }
+  }
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int m = (blockIdx.x * 32 + x) * V;
   const int lo = blockIdx.y * span, hi = min(t, lo + span);
@@ -37,9 +116,13 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
         load_vec(Z + (int64_t)n * ldz + m, z);
         act_grads<T, V>(d, z, act);
       }
-      if (WRITE) store_vec(dZ + (int64_t)n * lddz + m, d);
 #pragma unroll
       for (int i = 0; i < V; ++i) sum[i] += d[i];
+      if (WRITE) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] *= scale;
+        store_vec(dZ + (int64_t)n * lddz + m, d);
+      }
     }
   } else if (m < kn) {
     for (int n = lo + y; n < hi; n += 8) {
@@ -53,7 +136,7 @@ __global__ __launch_bounds__(256) void slope_kernel(int kn, int t, int span, con
             act_grads<T, 1>(&d, &z, act);
           }
         }
-        if (WRITE && m + i < lddz) dZ[(int64_t)n * lddz + m + i] = (T)d;
+        if (WRITE && m + i < lddz) dZ[(int64_t)n * lddz + m + i] = (T)(d * scale);
         sum[i] += d;
       }
     }
@@ -109,6 +192,9 @@ struct Layout {
   int64_t lddz = 0;            // kn rounded up to whole vectors
   int64_t part = 0;            // byte offset of the partial dbias
   int span = 0, parts = 0;
+  int cols = 0;                // workgroups of slope_kernel along the rows
+  int npeaks = 0;              // fp16 with a slope other than 0 and 1: the peaks,
+  int64_t peaks = 0;           // their byte offset, 1 / scale behind them
   int64_t product = 0;         // byte offset of the products' workspace
   int64_t bytes = 0;
 };
@@ -125,7 +211,10 @@ Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act
   if (w.own) d = Lines::kDirect;
   w.span = slope_span(dtype, kn, t);
   w.parts = (int)((t + w.span - 1) / w.span);
-  w.product = w.part + (w.parts > 1 ? up((int64_t)w.parts * kn * 4) : 0);
+  w.cols = (int)((kn + 32 * vec - 1) / (32 * vec));
+  w.peaks = w.part + (w.parts > 1 ? up((int64_t)w.parts * kn * 4) : 0);
+  if (dtype == LINEAR_F16 && act > LINEAR_ACT_RELU) w.npeaks = (int)std::min<int64_t>(kPeaks, (int64_t)w.cols * w.parts);
+  w.product = w.peaks + (w.npeaks ? up((w.npeaks + 1) * 4) : 0);
   w.bytes = w.product + std::max(product_workspace(dtype, f_order == 0, true, f, d, ci, t, kn),
                                  f_order ? product_workspace(dtype, false, false, x, d, ci, kn, t)
                                          : product_workspace(dtype, false, false, d, x, kn, ci, t));
@@ -134,13 +223,23 @@ Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act
 
 template <class T> hipError_t launch_slope(int64_t kn, int64_t t, const Layout& w, const void* dO, int64_t lddo, const void* Z,
                                            int64_t ldz, int act, char* ws, void* dbias, hipStream_t s) {
-  const dim3 grid((unsigned)((kn + 32 * kVec<T> - 1) / (32 * kVec<T>)), (unsigned)std::max(1, w.parts));
+  const dim3 grid((unsigned)w.cols, (unsigned)std::max(1, w.parts));
+  float* peaks = w.npeaks ? reinterpret_cast<float*>(ws + w.peaks) : nullptr;
+  if constexpr (std::is_same_v<T, f16>) {
+    if (peaks) {
+      peak_kernel<<<dim3((unsigned)w.npeaks), 256, 0, s>>>((int)kn, (int)t, w.span, w.cols, w.parts, static_cast<const T*>(dO), lddo,
+                                                           peaks);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
   auto k = act != LINEAR_ACT_NONE ? (dbias ? slope_kernel<T, true, true, true> : slope_kernel<T, true, true, false>)
            : w.own                ? (dbias ? slope_kernel<T, false, true, true> : slope_kernel<T, false, true, false>)
                                   : slope_kernel<T, false, false, true>;
   float* part = w.parts > 1 ? reinterpret_cast<float*>(ws + w.part) : nullptr;
   k<<<grid, 256, 0, s>>>((int)kn, (int)t, w.span, static_cast<const T*>(dO), lddo, static_cast<const T*>(Z), ldz, act,
-                         reinterpret_cast<T*>(ws), w.lddz, part, static_cast<T*>(dbias));
+                         reinterpret_cast<T*>(ws), w.lddz, part, static_cast<T*>(dbias), peaks, w.npeaks,
+                         peaks ? peaks + w.npeaks : nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !dbias || !part) return e;
   bias_kernel<T><<<dim3((unsigned)((kn + 31) / 32)), 256, 0, s>>>((int)kn, w.parts, part, static_cast<T*>(dbias));
@@ -200,6 +299,7 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
   }
   const void* dZ = w.own ? workspace : dO;
   const int64_t lddz = w.own ? w.lddz : lddo;
+  const float* back = w.npeaks ? reinterpret_cast<const float*>(ws + w.peaks) + w.npeaks : nullptr;
   const int dz_rows = (int)(w.own ? w.lddz : kn);      // as loaded: zeros follow in the library's own copy
   if (e == hipSuccess && dX) {
     Product p{};
@@ -211,6 +311,7 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.N = (int)t;
     p.K = (int)kn;
     p.bK = dz_rows;
+    p.e.scale = back;
     p.e.C = dX;
     p.e.ldc = lddx;
     e = launch_product(dtype, f_order == 0, true, p, ws + w.product, stream);
@@ -226,6 +327,7 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.N = (int)(f_order ? kn : ci);
     p.K = (int)t;
     (f_order ? p.brows : p.arows) = dz_rows;
+    p.e.scale = back;
     p.e.C = dF;
     p.e.ldc = lddf;
     e = launch_product(dtype, false, false, p, ws + w.product, stream);
