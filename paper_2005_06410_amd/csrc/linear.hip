@@ -974,8 +974,7 @@ template <class T, int W> hipError_t launch_ordered(bool a_kc, bool b_kc, Shape 
 }
 
 template <class T> hipError_t launch_typed(int dtype, bool a_kc, bool b_kc, Product p, char* ws, hipStream_t s) {
-  const Route r = route_of(dtype, a_kc, b_kc, lines_of(dtype, p.A, p.lda, a_kc ? p.aK : p.arows),
-                           lines_of(dtype, p.B, p.ldb, b_kc ? p.bK : p.brows), p.M, p.N, p.K);
+  const Route r = route_of(dtype, a_kc, b_kc, p.a, p.b, p.M, p.N, p.K);
   hipError_t e = hipSuccess;
   if (r.width == 0) {
     p.arows = p.M;
@@ -1112,12 +1111,13 @@ extern "C" int convgemm_linear(int dtype, int64_t kn, int64_t ci, int64_t t, con
   if (Z && bad_ld(ldz, kn)) return -15;
   if (!O && work) return -16;
   if (bad_ld(ldo, kn)) return -17;
-  const int64_t need = linear::product_workspace(dtype, f_order == 1, true, linear::lines_of(dtype, F, ldf, f_order ? ci : kn),
-                                                 linear::lines_of(dtype, X, ldx, ci), kn, t, ci);
+  linear::Product p{};
+  p.a = linear::lines_of(dtype, F, ldf, f_order ? ci : kn);
+  p.b = linear::lines_of(dtype, X, ldx, ci);
+  const int64_t need = linear::product_workspace(dtype, f_order == 1, true, p.a, p.b, kn, t, ci);
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 15))) return -18;
   if (need > 0 && workspace_bytes < need) return -19;
   if (!work) return LINEAR_OK;
-  linear::Product p{};
   p.A = F;
   p.lda = ldf;
   p.B = X;

@@ -141,6 +141,24 @@ template <class T, bool STREAM> __device__ inline void result_vec(T* p, const fl
   }
 }
 
+// An operand's lines (its contiguous extents): 16-byte aligned and whole 16 bytes
+// long, or not, or so far apart that a tile's offsets pass 32 bits.
+enum class Lines { kDirect, kRagged, kFar };
+constexpr Lines kAnyLines[] = {Lines::kDirect, Lines::kRagged, Lines::kFar};
+
+inline Lines lines_of(int dtype, const void* p, int64_t ld, int64_t len) {
+  const int64_t size = dtype == LINEAR_F32 ? 4 : 2;
+  if (ld * size * 512 >= (1ll << 32) - 4096) return Lines::kFar;
+  return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && len * size % 16 == 0 ? Lines::kDirect : Lines::kRagged;
+}
+
+// The same before addresses and leading dimensions are known, of lines that may be
+// next to each other.
+inline Lines lines_if(int dtype, bool aligned, int64_t len) {
+  const Lines l = lines_of(dtype, nullptr, len, len);
+  return l == Lines::kDirect && !aligned ? Lines::kRagged : l;
+}
+
 // What follows a product: C = act(product scale + bias) + residual, Z = product
 // scale + bias.
 struct Epilogue {
@@ -163,6 +181,7 @@ struct Product {
   int M, N, K;            // M, N >= 1
   int arows, aK;          // extents of the operands as they are loaded: M and K
   int brows, bK;          // (N and K), or more where zeros follow
+  Lines a, b;             // the operands' lines, as the workspace was sized for
   int splits;             // workgroups that share a tile's contraction
   int mtiles, ntiles;
   float* part;            // splits > 1: [splits][N][M] partial products
@@ -234,22 +253,6 @@ template <class T> __device__ inline void finish_one(const Epilogue& e, int m, i
 // linear.hip.  Where A's (B's) contiguous index is the contraction, a_kc (b_kc)
 // is set; its rows are then ld apart, else its contraction indices are.
 int compute_units();
-
-// An operand's lines (its contiguous extents): 16-byte aligned and whole 16 bytes
-// long, or not, or so far apart that a tile's offsets pass 32 bits.
-enum class Lines { kDirect, kRagged, kFar };
-constexpr Lines kAnyLines[] = {Lines::kDirect, Lines::kRagged, Lines::kFar};
-
-inline Lines lines_of(int dtype, const void* p, int64_t ld, int64_t len) {
-  const int64_t size = dtype == LINEAR_F32 ? 4 : 2;
-  if (ld * size * 512 >= (1ll << 32) - 4096) return Lines::kFar;
-  return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && len * size % 16 == 0 ? Lines::kDirect : Lines::kRagged;
-}
-
-// The same before addresses are known.
-inline Lines lines_if(int dtype, bool aligned, int64_t len) {
-  return aligned && len * (dtype == LINEAR_F32 ? 4 : 2) % 16 == 0 ? Lines::kDirect : Lines::kRagged;
-}
 
 // Bytes of workspace for a product.
 int64_t product_workspace(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int64_t N, int64_t K);

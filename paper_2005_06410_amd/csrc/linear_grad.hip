@@ -188,6 +188,7 @@ int slope_span(int dtype, int64_t kn, int64_t t) {
 
 // The workspace, in order.
 struct Layout {
+  Lines f, x, d;               // how the products' operands lie; d: dZ's lines, here or dO's own
   bool own = false;            // dZ is written here: an activation, or dO's lines are not direct
   int64_t lddz = 0;            // kn rounded up to whole vectors
   int64_t part = 0;            // byte offset of the partial dbias
@@ -206,9 +207,10 @@ Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act
   w.own = act != LINEAR_ACT_NONE || d == Lines::kFar || (d == Lines::kRagged && dtype != LINEAR_F32);
   if (w.own) {
     w.lddz = (kn + vec - 1) / vec * vec;
+    d = lines_of(dtype, nullptr, w.lddz, w.lddz);
     w.part = up(w.lddz * t * type_size(dtype));
   }
-  if (w.own) d = Lines::kDirect;
+  w.f = f, w.x = x, w.d = d;
   w.span = slope_span(dtype, kn, t);
   w.parts = (int)((t + w.span - 1) / w.span);
   w.cols = (int)((kn + 32 * vec - 1) / (32 * vec));
@@ -311,6 +313,8 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.N = (int)t;
     p.K = (int)kn;
     p.bK = dz_rows;
+    p.a = w.f;
+    p.b = w.d;
     p.e.scale = back;
     p.e.C = dX;
     p.e.ldc = lddx;
@@ -327,6 +331,8 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
     p.N = (int)(f_order ? kn : ci);
     p.K = (int)t;
     (f_order ? p.brows : p.arows) = dz_rows;
+    p.a = f_order ? w.x : w.d;
+    p.b = f_order ? w.d : w.x;
     p.e.scale = back;
     p.e.C = dF;
     p.e.ldc = lddf;
