@@ -41,7 +41,8 @@
  * at F[c + ldf k]).  Any leading dimension and any address that the type
  * allows are taken; operands whose addresses, leading dimensions or contiguous
  * extents are not multiples of 16 bytes cost narrower loads (fp32), a padded copy
- * (16-bit types) or, up to 64 tokens, loads through registers.
+ * (16-bit types) or, up to 64 tokens, loads through registers; so do lines of
+ * 2^22 fp32 or 2^23 16-bit values and more.
  *
  * Rules (as in ltlt.h): pointers are DEVICE pointers of the current HIP device
  * unless marked HOST; calls are stream-ordered and asynchronous; the caller

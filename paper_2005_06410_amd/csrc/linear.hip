@@ -106,6 +106,7 @@ template <class T, bool KC, int ROWS, int DEPTH, int NT, int WIDTH> struct Stage
   static constexpr int BYTES = ROWS * 128 * DEPTH;
   static_assert(PIECES * NT == ROWS * 8 * DEPTH * LANES, "whole pieces");
   static_assert(WIDTH == 0 || WIDTH == 16 || (WIDTH == 4 && sizeof(T) == 4), "load widths");
+  static_assert(WIDTH == 0 || (KC ? ROWS : BK * DEPTH) <= kStageLines, "32-bit offsets");
   const T* at;            // the tile's first row, next contraction index
   int64_t ld;
   int64_t left;           // values from `at` to the operand's last one
@@ -162,7 +163,7 @@ template <class T, bool KC, int ROWS, int DEPTH, int NT, int WIDTH> struct Stage
       // gives zero.  A KC row's pieces past the contraction's end lie inside
       // the next row and are sent out of range.
       const int64_t bytes = left * (int)sizeof(T);
-      const uint32_t range = !more || bytes <= 0 ? 0u : bytes > 0xfffff000ll ? 0xfffff000u : (uint32_t)bytes;
+      const uint32_t range = !more || bytes <= 0 ? 0u : bytes > kReach ? (uint32_t)kReach : (uint32_t)bytes;
       const i4 r = buffer_of(at, range);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
@@ -587,7 +588,7 @@ template <class T, bool KC, int SR> struct WideStage {
     const T* b = base + (KC ? (int64_t)k0 : (int64_t)k0 * ld);
     const int64_t span = KC ? (int64_t)(min(rows, 256) - 1) * ld + (K - k0) : (int64_t)(min(K - k0, BK) - 1) * ld + rows;
     const uint64_t bytes = (uint64_t)span * SIZE;
-    const uint32_t range = kt >= end ? 0u : bytes > 0xfffff000u ? 0xfffff000u : (uint32_t)bytes;
+    const uint32_t range = kt >= end ? 0u : bytes > (uint64_t)kReach ? (uint32_t)kReach : (uint32_t)bytes;
     r = buffer_of(b, range);
     mask = KC && first >= K - k0 ? 0xffffffffu : 0u;
   }
@@ -883,9 +884,21 @@ Plan plan_of(int dtype, int width, bool a_kc, bool b_kc, int64_t M, int64_t N, i
   return e.plan;
 }
 
-int register_splits(int dtype, int64_t M, int64_t N, int64_t K) {
-  const int64_t stages = ceil_div(K, 4 * (dtype == LINEAR_F32 ? 32 : 64)), tiles = ceil_div(M, 64);
-  return M > 0 && N > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>({compute_units() / tiles, stages / 4, 16})) : 1;
+// The tile of the kernels that load through registers, and how often its
+// contraction is split: until every compute unit has a workgroup, each with four
+// stages at least; 16 times at most, but for a contraction of millions of values.
+struct RegisterTile {
+  int m, n, depth;
+};
+RegisterTile register_tile(bool b_kc, int64_t N) {
+  return N > 64 ? RegisterTile{128, 128, 1} : b_kc && N <= 16 ? RegisterTile{64, 16, 4} : RegisterTile{64, 64, 4};
+}
+
+int register_splits(int dtype, bool b_kc, int64_t M, int64_t N, int64_t K) {
+  if (M <= 0 || N <= 0) return 1;
+  const RegisterTile t = register_tile(b_kc, N);
+  const int64_t stages = ceil_div(K, t.depth * (dtype == LINEAR_F32 ? 32 : 64)), tiles = ceil_div(M, t.m) * ceil_div(N, t.n);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({compute_units() / tiles, stages / 4, K < 1 << 21 ? 16 : 256}));
 }
 
 int64_t padded(int dtype, int64_t n) { return dtype == LINEAR_F32 ? (n + 3) / 4 * 4 : (n + 7) / 8 * 8; }
@@ -895,7 +908,9 @@ int64_t copy_values(int dtype, bool kc, int64_t rows, int64_t K) { return kc ? r
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// How operands reach LDS: directly where their lines are direct.  Else, for few
+// How operands reach LDS: directly where their lines are direct.  Through
+// registers, with 64-bit addresses, where even a copy's lines would be too long for
+// the direct loads (from 2^22 fp32 or 2^23 16-bit values on).  Else, for few
 // columns of 16-bit types, through registers (a copy would triple what is read of
 // an operand that is read about once); for fp32 by loads of single values, from
 // any address, where the figures above say that this is faster than a padded
@@ -908,6 +923,8 @@ struct Route {
 Route route_of(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int64_t N, int64_t K) {
   const Route copied{16, a != Lines::kDirect, b != Lines::kDirect};
   if (!copied.copy_a && !copied.copy_b) return copied;
+  auto long_lines = [&](int64_t len) { return lines_of(dtype, nullptr, padded(dtype, len), padded(dtype, len)) == Lines::kFar; };
+  if (long_lines(a_kc ? K : M) || long_lines(b_kc ? K : N)) return Route{0, false, false};
   if (dtype == LINEAR_F32 && a != Lines::kFar && b != Lines::kFar) {
     const int64_t values = (copied.copy_a ? copy_values(dtype, a_kc, M, K) : 0) + (copied.copy_b ? copy_values(dtype, b_kc, N, K) : 0);
     const double copy = 5.0 + 2.0 * 4.0 * values / kRates32.read;
@@ -962,9 +979,12 @@ template <class T, bool AKC, bool BKC, int W> hipError_t launch_shape(Shape shap
   return launch_ring<Ring<T, AKC, BKC, 4, 4, 2, 2, 1, 1, 2, W>>(p, s);
 }
 
-template <class T, bool AKC> hipError_t launch_registers(const Product& p, hipStream_t s) {
-  if (p.N <= 16) return launch_ring<Ring<T, AKC, true, 4, 1, 1, 1, 4, 4, 2, 0>>(p, s);
-  return launch_ring<Ring<T, AKC, true, 4, 4, 1, 1, 4, 4, 2, 0>>(p, s);
+template <class T, bool AKC, bool BKC> hipError_t launch_registers(const Product& p, hipStream_t s) {
+  if (p.N > 64) return launch_ring<Ring<T, AKC, BKC, 4, 4, 2, 2, 1, 1, 2, 0>>(p, s);
+  if constexpr (BKC) {
+    if (p.N <= 16) return launch_ring<Ring<T, AKC, BKC, 4, 1, 1, 1, 4, 4, 2, 0>>(p, s);
+  }
+  return launch_ring<Ring<T, AKC, BKC, 4, 4, 1, 1, 4, 4, 2, 0>>(p, s);
 }
 
 template <class T, int W> hipError_t launch_ordered(bool a_kc, bool b_kc, Shape shape, const Product& p, hipStream_t s) {
@@ -980,9 +1000,11 @@ template <class T> hipError_t launch_typed(int dtype, bool a_kc, bool b_kc, Prod
     p.arows = p.M;
     p.brows = p.N;
     p.aK = p.bK = p.K;
-    p.splits = register_splits(dtype, p.M, p.N, p.K);
+    p.splits = register_splits(dtype, b_kc, p.M, p.N, p.K);
     p.part = reinterpret_cast<float*>(ws);
-    e = a_kc ? launch_registers<T, true>(p, s) : launch_registers<T, false>(p, s);
+    e = a_kc   ? launch_registers<T, true, true>(p, s)
+        : b_kc ? launch_registers<T, false, true>(p, s)
+               : launch_registers<T, false, false>(p, s);
   } else {
     const Plan plan = plan_of(dtype, r.width, a_kc, b_kc, p.M, p.N, p.K);
     p.splits = plan.splits;
@@ -1033,7 +1055,8 @@ void product_choice(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M
   }
   const Route r = route_of(dtype, a_kc, b_kc, a, b, M, N, K);
   if (r.width == 0) {
-    out[0] = 4, out[1] = 64, out[2] = N <= 16 ? 16 : 64, out[3] = register_splits(dtype, M, N, K), out[4] = 0, out[5] = 0;
+    const RegisterTile t = register_tile(b_kc, N);
+    out[0] = 4, out[1] = t.m, out[2] = t.n, out[3] = register_splits(dtype, b_kc, M, N, K), out[4] = 0, out[5] = 0;
   } else {
     const Plan p = plan_of(dtype, r.width, a_kc, b_kc, M, N, K);
     const Tile& t = kTiles[p.shape];
@@ -1047,7 +1070,7 @@ int64_t product_workspace(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int
   int64_t bytes = 0;
   if (r.copy_a) bytes += up256(copy_values(dtype, a_kc, M, K) * type_size(dtype));
   if (r.copy_b) bytes += up256(copy_values(dtype, b_kc, N, K) * type_size(dtype));
-  const int64_t splits = r.width == 0 ? register_splits(dtype, M, N, K) : plan_of(dtype, r.width, a_kc, b_kc, M, N, K).splits;
+  const int64_t splits = r.width == 0 ? register_splits(dtype, b_kc, M, N, K) : plan_of(dtype, r.width, a_kc, b_kc, M, N, K).splits;
   return bytes + (splits > 1 ? splits * M * N * 4 : 0);
 }
 

@@ -142,13 +142,17 @@ template <class T, bool STREAM> __device__ inline void result_vec(T* p, const fl
 }
 
 // An operand's lines (its contiguous extents): 16-byte aligned and whole 16 bytes
-// long, or not, or so far apart that a tile's offsets pass 32 bits.
+// long, or not, or so far apart that a tile's offsets do not fit the direct loads.
 enum class Lines { kDirect, kRagged, kFar };
 constexpr Lines kAnyLines[] = {Lines::kDirect, Lines::kRagged, Lines::kFar};
 
+// Most lines of an operand that one stage of a tile spans, and the bytes that its
+// loads reach (32-bit offsets, below those that say "nowhere").
+constexpr int64_t kStageLines = 256, kReach = 0xfffff000ll;
+
 inline Lines lines_of(int dtype, const void* p, int64_t ld, int64_t len) {
   const int64_t size = dtype == LINEAR_F32 ? 4 : 2;
-  if (ld * size * 512 >= (1ll << 32) - 4096) return Lines::kFar;
+  if (ld * size * kStageLines > kReach) return Lines::kFar;
   return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && len * size % 16 == 0 ? Lines::kDirect : Lines::kRagged;
 }
 

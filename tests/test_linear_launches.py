@@ -136,3 +136,53 @@ def test_everything_stays_inside(lib, dtype):
         calls.append(backward(lib, dtype, kn, ci, t, order, rng.randrange(5), pad, shift))
     for (need, call), (code, launched) in zip(calls, launches.record([c for _, c in calls])):
         check_inside(need, call, code, launched)
+
+
+def ring_of(name):
+    """A direct-loading kernel's operands as (contraction contiguous, lines of a
+    stage, values of a line that a stage reaches), and the bytes of a value; None
+    where the kernel loads through registers."""
+    bits = {"float": 4, "unsigned short": 2, "short": 2}
+    if m := re.search(r"wide_kernel<([\w ]+), (\w+), (\w+), \w+>", name):
+        size = bits[m[1]]
+        return size, [(True, 256, 64) if m[k] == "true" else (False, 64, 256) for k in (2, 3)]
+    m = re.search(r"Ring<([\w ]+), (\w+), (\w+), ([\d, ]+)>", name)
+    size = bits[m[1]]
+    wm, wn, waves_m, waves_n, _, depth, _, width = (int(v) for v in m[4].split(","))
+    if width == 0:
+        return None
+    deep = 128 // size * depth
+    return size, [(True, rows, deep) if m[k] == "true" else (False, deep, rows)
+                  for k, rows in ((2, 16 * wm * waves_m), (3, 16 * wn * waves_n))]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_offsets_fit_the_direct_loads(lib, dtype):
+    """The 32-bit offsets of a stage, its lanes beyond the operand's end among them,
+    lie below the range that says "nowhere"; launches hold fewer than 2^32 threads."""
+    rng = random.Random(dtype + 100)
+    sizes = [(long, a, b) for long in EDGES for a, b in [(1024, 1024), (512, 512), (64, 80), (8, 8), (200, 1), (3000, 24), (260, 3), (8, 8192), (8192, 1), (1, 4000)]]
+    sizes += [(int(2 ** rng.uniform(20, 24)) - 1, int(2 ** rng.uniform(0, 11)), int(2 ** rng.uniform(0, 11))) for _ in range(60)]
+    calls = []
+    for long, a, b in sizes:
+        for kn, ci, t in [(long, a, b), (a, long, b), (a, b, long)]:
+            for order in (0, 1):
+                for pad in {0, min(1 << 20, LIMIT - 1 - long), min(1 << 23, LIMIT - 1 - long)}:
+                    calls.append(forward(lib, dtype, kn, ci, t, order, pad))
+                    calls.append(backward(lib, dtype, kn, ci, t, order, 0, pad))
+                calls.append(backward(lib, dtype, kn, ci, t, order, 2))
+    seen = set()
+    for (need, call), (code, launched) in zip(calls, launches.record([c for _, c in calls])):
+        check_inside(need, call, code, launched)
+        for v in launched:
+            assert v["grid"] * v["block"] < 1 << 32, (call, v)
+            if kind(v) not in ("ring_kernel", "wide_kernel"):
+                continue
+            ring = ring_of(v["kernel"])
+            seen.add(ring is None)
+            if ring is None:
+                continue
+            size, operands = ring
+            for (kc, lines, reach), ld in zip(operands, (v["lda"], v["ldb"])):
+                assert ((lines - 1) * ld + reach) * size < 0xfffff000, (call, v)
+    assert seen == {True, False}
