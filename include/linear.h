@@ -121,7 +121,7 @@ int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, in
                                            int aligned);
 
 /* dX, dF and dbias from dO; each of the three may be NULL and is then not
- * computed.  F may be NULL where dX is, X where dF is.  Z is the pre-activation
+ * computed (the bytes that the query names are enough all the same).  F may be NULL where dX is, X where dF is.  Z is the pre-activation
  * that convgemm_linear wrote; it is not looked at where act is LINEAR_ACT_NONE.
  * dF has F's order; its leading dimension is lddf. */
 int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order, int64_t ldf,

@@ -186,10 +186,11 @@ int slope_span(int dtype, int64_t kn, int64_t t) {
   return (int)(t <= 128 ? std::max<int64_t>(t, 1) : std::max<int64_t>(32, (t + parts - 1) / parts));
 }
 
-// The workspace, in order.
+// The workspace, in order, for the outputs that are wanted: one that is left out
+// never adds to it.
 struct Layout {
   Lines f, x, d;               // how the products' operands lie; d: dZ's lines, here or dO's own
-  bool own = false;            // dZ is written here: an activation, or dO's lines are not direct
+  bool own = false;            // dZ is written here: a product wants it, and there is an activation or dO's lines are not direct
   int64_t lddz = 0;            // kn rounded up to whole vectors
   int64_t part = 0;            // byte offset of the partial dbias
   int span = 0, parts = 0;
@@ -200,11 +201,13 @@ struct Layout {
   int64_t bytes = 0;
 };
 
-Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act, Lines f, Lines x, Lines d) {
+Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act, Lines f, Lines x, Lines d, bool want_dx,
+              bool want_df) {
   auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
   const int64_t vec = 16 / type_size(dtype);
   Layout w;
-  w.own = act != LINEAR_ACT_NONE || d == Lines::kFar || (d == Lines::kRagged && dtype != LINEAR_F32);
+  w.own = (want_dx || want_df) &&
+          (act != LINEAR_ACT_NONE || d == Lines::kFar || (d == Lines::kRagged && dtype != LINEAR_F32));
   if (w.own) {
     w.lddz = (kn + vec - 1) / vec * vec;
     d = lines_of(dtype, nullptr, w.lddz, w.lddz);
@@ -215,11 +218,14 @@ Layout layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int act
   w.parts = (int)((t + w.span - 1) / w.span);
   w.cols = (int)((kn + 32 * vec - 1) / (32 * vec));
   w.peaks = w.part + (w.parts > 1 ? up((int64_t)w.parts * kn * 4) : 0);
-  if (dtype == LINEAR_F16 && act > LINEAR_ACT_RELU) w.npeaks = (int)std::min<int64_t>(kPeaks, (int64_t)w.cols * w.parts);
+  if (w.own && dtype == LINEAR_F16 && act > LINEAR_ACT_RELU) w.npeaks = (int)std::min<int64_t>(kPeaks, (int64_t)w.cols * w.parts);
   w.product = w.peaks + (w.npeaks ? up((w.npeaks + 1) * 4) : 0);
-  w.bytes = w.product + std::max(product_workspace(dtype, f_order == 0, true, f, d, ci, t, kn),
-                                 f_order ? product_workspace(dtype, false, false, x, d, ci, kn, t)
-                                         : product_workspace(dtype, false, false, d, x, kn, ci, t));
+  int64_t most = 0;
+  if (want_dx) most = product_workspace(dtype, f_order == 0, true, f, d, ci, t, kn);
+  if (want_df)
+    most = std::max(most, f_order ? product_workspace(dtype, false, false, x, d, ci, kn, t)
+                                  : product_workspace(dtype, false, false, d, x, kn, ci, t));
+  w.bytes = w.product + most;
   return w;
 }
 
@@ -235,9 +241,12 @@ template <class T> hipError_t launch_slope(int64_t kn, int64_t t, const Layout& 
       if (e != hipSuccess) return e;
     }
   }
-  auto k = act != LINEAR_ACT_NONE ? (dbias ? slope_kernel<T, true, true, true> : slope_kernel<T, true, true, false>)
-           : w.own                ? (dbias ? slope_kernel<T, false, true, true> : slope_kernel<T, false, true, false>)
-                                  : slope_kernel<T, false, false, true>;
+  auto k = act != LINEAR_ACT_NONE ? (!w.own ? slope_kernel<T, true, false, true>
+                                    : dbias ? slope_kernel<T, true, true, true>
+                                            : slope_kernel<T, true, true, false>)
+           : !w.own ? slope_kernel<T, false, false, true>
+           : dbias  ? slope_kernel<T, false, true, true>
+                    : slope_kernel<T, false, true, false>;
   float* part = w.parts > 1 ? reinterpret_cast<float*>(ws + w.part) : nullptr;
   k<<<grid, 256, 0, s>>>((int)kn, (int)t, w.span, static_cast<const T*>(dO), lddo, static_cast<const T*>(Z), ldz, act,
                          reinterpret_cast<T*>(ws), w.lddz, part, static_cast<T*>(dbias), peaks, w.npeaks,
@@ -259,11 +268,11 @@ extern "C" int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int
   using namespace linear;
   if (aligned)
     return layout(dtype, kn, ci, t, f_order, act, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci),
-                  lines_if(dtype, true, kn)).bytes;
+                  lines_if(dtype, true, kn), true, true).bytes;
   int64_t most = 0;
   for (Lines f : kAnyLines)
     for (Lines x : kAnyLines)
-      for (Lines d : kAnyLines) most = std::max(most, layout(dtype, kn, ci, t, f_order, act, f, x, d).bytes);
+      for (Lines d : kAnyLines) most = std::max(most, layout(dtype, kn, ci, t, f_order, act, f, x, d, true, true).bytes);
   return most;
 }
 
@@ -285,9 +294,9 @@ extern "C" int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64
   if (act != LINEAR_ACT_NONE && bad_ld(ldz, kn)) return -13;
   if (dX && bad_ld(lddx, ci)) return -16;
   if (dF && bad_ld(lddf, f_order ? ci : kn)) return -18;
-  const Layout w = layout(dtype, kn, ci, t, f_order, act, 
+  const Layout w = layout(dtype, kn, ci, t, f_order, act,
                           dX ? lines_of(dtype, F, ldf, f_order ? ci : kn) : Lines::kDirect,
-                          dF ? lines_of(dtype, X, ldx, ci) : Lines::kDirect, lines_of(dtype, dO, lddo, kn));
+                          dF ? lines_of(dtype, X, ldx, ci) : Lines::kDirect, lines_of(dtype, dO, lddo, kn), dX, dF);
   if (w.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return -20;
   if (workspace_bytes < w.bytes) return -21;
   char* ws = static_cast<char*>(workspace);

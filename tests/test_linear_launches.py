@@ -186,3 +186,31 @@ def test_offsets_fit_the_direct_loads(lib, dtype):
             for (kc, lines, reach), ld in zip(operands, (v["lda"], v["ldb"])):
                 assert ((lines - 1) * ld + reach) * size < 0xfffff000, (call, v)
     assert seen == {True, False}
+
+
+SUBSETS = [(1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_fewer_outputs_need_no_more(lib, dtype):
+    """The bytes that the query names are enough whatever outputs are left out; with
+    dbias alone nothing else is written."""
+    rng = random.Random(dtype + 200)
+    calls = []
+    sizes = [(2070, 246, 52), (5361, 186, 7)] + [tuple(int(2 ** rng.uniform(0, 13)) for _ in range(3)) for _ in range(250)]
+    for kn, ci, t in sizes:
+        order, act, vec = rng.randrange(2), rng.choice([0, 0, 1, 2]), 16 // SIZE[dtype]
+        # leading dimensions of whole vectors, extents of any length
+        lds = [up(n, vec) for n in (ci if order else kn, ci, kn)]
+        for needs in SUBSETS:
+            need, (name, args) = backward(lib, dtype, kn, ci, t, order, act, needs=needs)
+            args = list(args)
+            args[6], args[8], args[10], args[12] = lds[0], lds[1], lds[2], lds[2]
+            need = args[-2] = lib.convgemm_linear_backward_workspace(dtype, kn, ci, t, order, act, 1)
+            calls.append((needs, need, (name, tuple(args))))
+    for (needs, need, call), (code, launched) in zip(calls, launches.record([c for _, _, c in calls])):
+        check_inside(need, call, code, launched)
+        if needs == (0, 0, 1):
+            assert {kind(v) for v in launched} <= {"slope_kernel", "bias_kernel"} and not any(v.get("lddz") for v in launched)
+        if needs == (0, 0, 0):
+            assert not launched
