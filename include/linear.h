@@ -20,8 +20,11 @@
  *
  * Clipping.  Over all tensors g together,
  *        norm = sqrt(sum g^2),   c = min(1, max_norm / norm),   out = c g,
- * with c = 1 where norm = 0.  An infinite norm gives c = 0 and a NaN norm a NaN
- * c, as the formula says; the caller reads norm where that matters.
+ * with c = 1 where norm = 0.  norm and c are computed in fp64, c is applied to
+ * fp32's precision at any size, and norm is returned in fp32: one above that range
+ * is returned as infinity, though c goes by its value.  An infinite or NaN gradient
+ * gives c = 0 or a NaN c, as the formula says; the caller reads norm where that
+ * matters.
  *
  * Types: LINEAR_F32, LINEAR_BF16, LINEAR_F16; all tensors of one layer have the
  * same type.  Products are summed in fp32 on the matrix cores and the epilogue

@@ -707,7 +707,8 @@ def clip_grad_norm(grads, max_norm: float, out=None):
     sizes, types and order in memory).  Returns the norm before scaling, as
     ``grad_norm`` does; nothing is copied to the host.
 
-    An infinite norm makes c zero and a NaN norm makes it NaN.  The tensors to be
+    An infinite gradient makes c zero and a NaN makes it NaN; a norm above fp32's
+    range is returned as infinity but scales by its value.  The tensors to be
     scaled may not overlap one another (the same one twice is refused)."""
     if not max_norm >= 0:
         raise ValueError("max_norm must be at least 0")

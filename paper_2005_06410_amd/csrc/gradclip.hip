@@ -100,7 +100,22 @@ template <class T> __device__ inline double squares(const T* g, int64_t n) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-template <bool STREAM, class T> __device__ inline void scale(const T* g, T* out, int64_t n, float c) {
+// c = m 2^e: e = 0 where c is a normal fp32 value (or 0, 1 or NaN), and m in [1/2, 1)
+// where it is smaller, since a large gradient times such a c is a normal value again.
+struct Factor {
+  float m;
+  int e;
+};
+
+__device__ inline Factor factor_of(double norm, double max_norm) {
+  if (norm <= max_norm) return Factor{1.0f, 0};
+  const double c = max_norm / norm;                  // a NaN norm gives a NaN factor
+  int e = 0;
+  const double m = c > 0.0 && c < 0x1p-126 ? frexp(c, &e) : c;
+  return Factor{(float)m, e};
+}
+
+template <bool STREAM, class T> __device__ inline void scale(const T* g, T* out, int64_t n, Factor c) {
   constexpr int V = kVec<T>;
   for_values<T>(
       n,
@@ -112,11 +127,11 @@ template <bool STREAM, class T> __device__ inline void scale(const T* g, T* out,
 #pragma unroll
         for (int u = 0; u < C; ++u) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) v[u][j] *= c;
+          for (int j = 0; j < V; ++j) v[u][j] = ldexpf(v[u][j] * c.m, c.e);
           result_vec<T, STREAM>(out + (int64_t)(i + 256 * u) * V, v[u]);
         }
       },
-      [&](int i) { out[i] = (T)((float)g[i] * c); });
+      [&](int i) { out[i] = (T)ldexpf((float)g[i] * c.m, c.e); });
 }
 
 // Calls f(tensor, first value, values) for the chunks lo .. hi-1, one at a time,
@@ -166,12 +181,11 @@ template <bool STREAM>
 __global__ __launch_bounds__(256) void scale_kernel(List l, const double* part, int parts, double max_norm, float* norm) {
   const double v = total_norm(part, parts);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-  // a NaN norm gives a NaN factor
-  const float c = v <= max_norm ? 1.0f : (float)(max_norm / v);
+  const Factor c = factor_of(v, max_norm);
   const int chunks = l.first[l.count];
   const int lo = (int)((int64_t)chunks * blockIdx.x / gridDim.x), hi = (int)((int64_t)chunks * (blockIdx.x + 1) / gridDim.x);
   for_chunks<true>(l, lo, hi, [&](int i, int64_t at, int64_t n) {
-    if (c == 1.0f && l.out[i] == l.g[i]) return;
+    if (c.m == 1.0f && c.e == 0 && l.out[i] == l.g[i]) return;
     if (l.dtype[i] == LINEAR_F32)
       scale<STREAM>(static_cast<const float*>(l.g[i]) + at, static_cast<float*>(l.out[i]) + at, n, c);
     else if (l.dtype[i] == LINEAR_BF16)
