@@ -27,14 +27,14 @@ namespace linear {
 namespace {
 
 constexpr int kList = 240;          // tensors of one launch: the list travels in the kernel's arguments
-constexpr int64_t kTensorLimit = 1ll << 37;   // values of one tensor: the chunks of a list are below 2^31
+constexpr int64_t kTensorLimit = 1ll << 37;   // values of one tensor
 constexpr int kParts = 2048;        // partial sums (workgroups of the first pass)
 // Above this the scaled values are stored past the caches: what of the gradients
 // is still in the last-level cache stays there for the second pass (200 bf16
 // tensors, 180 MB: 99 -> 90 us).
 constexpr int64_t kStream = 128ll << 20;
 constexpr int kMinChunk = 4096;     // bytes that a workgroup takes at a time: one vector per thread ..
-constexpr int kMaxChunk = 32768;    // .. to eight
+constexpr int kMaxChunk = 32768;    // .. to eight; larger ones where a list would have 2^30 chunks
 
 struct List {
   const void* g[kList];
@@ -213,17 +213,22 @@ int take(List& l, int chunk, int from, int count, const void* const* g, void* co
   return from;
 }
 
+// Bytes of all tensors, or 2^60 where they are more (a norm may count one tensor
+// any number of times).
 int64_t bytes_of(int count, const int64_t* n, const int* dtype) {
+  constexpr int64_t most = 1ll << 60;
   int64_t bytes = 0;
-  for (int i = 0; i < count; ++i) bytes += n[i] * type_size(dtype[i]);
-  return bytes;
+  for (int i = 0; i < count && bytes < most; ++i) bytes += n[i] * type_size(dtype[i]);
+  return std::min(bytes, most);
 }
 
 // Bytes of a chunk: as large as leaves every one of the first pass's workgroups
-// a chunk.
+// a chunk.  A list holds kList kTensorLimit values at most, 2^47 bytes: with chunks
+// of 2^30 bytes it has fewer than 2^31 chunks in any case.
 int chunk_of(int64_t bytes) {
   int chunk = kMinChunk;
   while (chunk < kMaxChunk && bytes / (2 * chunk) >= kParts) chunk *= 2;
+  while (chunk < 1 << 30 && bytes / chunk >= 1ll << 30) chunk *= 2;
   return chunk;
 }
 

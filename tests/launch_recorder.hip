@@ -34,6 +34,16 @@ struct Copy {
   int len;
 };
 
+// As in gradclip.hip.
+struct List {
+  const void* g[240];
+  void* out[240];
+  int64_t n[240];
+  int first[241];
+  unsigned char dtype[240];
+  int count, chunk;
+};
+
 void put(const char* key, int64_t v) { text += ", \"" + std::string(key) + "\": " + std::to_string(v); }
 void put(const char* key, const void* p) { put(key, (int64_t)(uintptr_t)p); }
 
@@ -107,6 +117,14 @@ SHOWN hipError_t hipLaunchKernel(const void* host, dim3 grid, dim3 block, void**
     put("span", (int64_t)*static_cast<const int*>(args[2]));
     put("dZ", *static_cast<void* const*>(args[8])), put("lddz", *static_cast<const int64_t*>(args[9]));
     put("part", *static_cast<void* const*>(args[10])), put("dbias", *static_cast<void* const*>(args[11]));
+  }
+  if (is("norm_kernel") || is("scale_kernel")) {
+    const List& l = *static_cast<const List*>(args[0]);
+    put("count", (int64_t)l.count), put("chunk", (int64_t)l.chunk);
+    // the chunks of each tensor, by the numbers before it and before the next
+    text += ", \"chunks\": [";
+    for (int i = 0; i < l.count; ++i) text += (i ? ", " : "") + std::to_string((int64_t)l.first[i + 1] - l.first[i]);
+    text += "], \"last\": " + std::to_string(l.first[l.count]);
   }
   text += "}\n";
   return hipSuccess;
