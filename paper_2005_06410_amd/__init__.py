@@ -506,6 +506,29 @@ def _columns(v, rows: int, cols: int, name: str, dtype, dev: int) -> int:
     return s1 if cols > 1 else max(rows, 1)
 
 
+def _meet(a: int, alen: int, alines: int, ald: int, b: int, blen: int, blines: int, bld: int) -> bool:
+    """Whether two sets of lines share a value: lines of `len` values, `ld` apart,
+    from the addresses a and b (in values).  Lines at different distances, both with
+    gaps, are taken for disjoint."""
+    if alen * alines == 0 or blen * blines == 0:
+        return False
+    if a + (alines - 1) * ald + alen <= b or b + (blines - 1) * bld + blen <= a:
+        return False
+    if alines == 1 or ald == alen:                   # a has no gaps: one line
+        alen, alines = (alines - 1) * ald + alen, 1
+    if blines == 1 or bld == blen:
+        blen, blines = (blines - 1) * bld + blen, 1
+    if blines == 1:
+        a, alen, alines, ald, b, blen, blines, bld = b, blen, blines, bld, a, alen, alines, ald
+    if alines == 1:                                  # the first line of b that ends behind a's start
+        k = 0 if b + blen > a else (a - b - blen) // bld + 1
+        return k < blines and b + k * bld < a + alen
+    if ald != bld:
+        return False
+    d = (b - a) % ald                                # within the same period
+    return d < alen or d + blen > ald
+
+
 def _weights(F, ci: int, dtype, dev: int):
     """(kn, order, leading dimension) of weights with either index fastest."""
     if F.dim() != 2:
@@ -577,8 +600,10 @@ def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, k
     gelu_tanh or silu.
 
     Returns O (kn, t) in the same storage (``out`` if given; it may be
-    ``residual`` itself), or (O, Z) with the pre-activation
-    Z = F X + bias for ``linear_backward`` where ``keep_pre`` is set."""
+    ``residual`` itself and overlap no other input), or (O, Z) with the pre-activation
+    Z = F X + bias for ``linear_backward`` where ``keep_pre`` is set.  Nothing is
+    recorded for torch's automatic differentiation, whatever the tensors require:
+    gradients come from ``linear_backward``."""
     ci, t, ldx, dtype, code, dev = _layer_input(X)
     kn, order, ldf = _weights(F, ci, dtype, dev)
     act = _activation(activation)
@@ -600,6 +625,11 @@ def linear(F, X, bias=None, activation: str = "none", residual=None, out=None, k
         ldo = max(kn, 1)
     else:
         ldo = _columns(out, kn, t, "out", dtype, dev)
+        size, op = out.element_size(), out.data_ptr()
+        inputs = [(X.data_ptr(), ci, t, ldx), (F.data_ptr(), *((ci, kn) if order else (kn, ci)), ldf), (bp, kn if bp else 0, 1, 1),
+                  (rp, kn if rp and not (rp == op and ldr == ldo) else 0, t, ldr)]
+        if any([_meet(op // size, kn, t, ldo, p // size, rows, lines, ld) for p, rows, lines, ld in inputs]):
+            raise ValueError("out may not overlap an input other than residual itself")
     if keep_pre:
         Z = X.new_empty_strided((kn, t), (1, max(kn, 1)))
         zp = Z.data_ptr()
@@ -724,9 +754,14 @@ def _norm_and_clip(grads, max_norm, out):
                 [o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))
                  for o, g in zip(outs, grads)])):
             raise ValueError("out must have the gradients' sizes, types, order in memory and GPU")
-    if max_norm is not None and len(set(optrs)) != len(optrs) and len(
-            {p for p, n in zip(optrs, sizes) if n}) != len(sizes) - sizes.count(0):
-        raise ValueError("a tensor to be scaled is named twice")
+    if max_norm is not None:
+        names = set(optrs)
+        if len(names) != len(optrs) and len({p for p, n in zip(optrs, sizes) if n}) != len(sizes) - sizes.count(0):
+            raise ValueError("a tensor to be scaled is named twice")
+        if out is not None and not names.isdisjoint(ptrs):
+            where = {p: i for i, (p, n) in enumerate(zip(ptrs, sizes)) if n}
+            if any(n and where.get(p, i) != i for i, (p, n) in enumerate(zip(optrs, sizes))):
+                raise ValueError("an output is another gradient")
     norm = grads[0].new_empty((), dtype=_torch().float32)
     count = len(grads)
     need = _scratch_bytes("convgemm_grad_workspace", dev, count)
