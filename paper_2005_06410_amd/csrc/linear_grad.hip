@@ -32,7 +32,8 @@ __device__ inline float wave_max(float v) {
 }
 
 // The largest finite |dO| of each workgroup's part, the parts as in slope_kernel.
-// One more read of dO (8192 tokens of 4096 rows: 67 MB).
+// One more read of dO, bound by memory and for small ones by latency: 4096 tokens of
+// 16384 rows 27 us (4.9 TB/s), 777 of 1001 3.7 us.
 __global__ __launch_bounds__(256) void peak_kernel(int kn, int t, int span, int cols, int parts, const f16* __restrict__ dO,
                                                    int64_t lddo, float* __restrict__ peaks) {
   constexpr int V = kVec<f16>;
