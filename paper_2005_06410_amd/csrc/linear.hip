@@ -404,7 +404,8 @@ template <class T> __device__ inline Operand<T> operand_b(const Product& p) {
 // multiplied, so STAGES - 1 stages are under way at any time.  For few tokens the
 // bound is the bytes under way: 16384 x 4096 bf16 weights by 8 tokens run at 5.6 TB/s
 // with 73 KB per compute unit, at 3.5 with 27; for tens to hundreds of tokens it is
-// what the L2 caches deliver (about 12 TB/s) and a stage's own latencies (0.3 us).
+// what the L2 caches deliver (8 to 9 TB/s at 80 and at 300 tokens) and a stage's own
+// latencies (0.3 us).
 template <class T, bool AKC, bool BKC, int WM, int WN, int WAVES_M, int WAVES_N, int WAVES_K, int DEPTH, int STAGES, int WIDTH>
 struct Ring {
   static constexpr bool DMA = WIDTH > 0;
@@ -535,10 +536,11 @@ template <class R> __global__ __launch_bounds__(R::NT, 2) void ring_kernel(Produ
 // phase) always means: what the next phase reads is there, and every load has
 // four phases to arrive. The upper four waves run one barrier behind the
 // lower four, so that on every SIMD one wave reads while the other multiplies.
-// 8192^3 bf16: 1406 TFLOP/s with the contraction contiguous in both operands, 1350
-// and 1332 with one and none, 5 % less on a slower card (library product: 1411, 1227,
-// 1086; the 128 x 128 ring: 1050 at 4096^3).  Bound by the matrix cores at the clock that they hold; between
-// tiles, by the results, which are written while no product runs.
+// 8192^3 bf16: 1430 TFLOP/s with the contraction contiguous in both operands, 1378
+// and 1353 with one and none (the library's product in turn on the same card: 1645,
+// 1407 and 1229; cards differ by 5 %); the 128 x 128 ring: 1050 at 4096^3.  Bound by
+// the matrix cores at the clock that they hold; between tiles, by the results, which
+// are written while no product runs.
 // One operand of the wide product: sub-tiles of SR rows (64 of A, 32 of B) x
 // 128 bytes, each as in Stage. Half h of the operand is the sub-tiles 2 s + h.
 template <class T, bool KC, int SR> struct WideStage {

@@ -92,3 +92,38 @@ def test_all_zero():
     F, X, z = (place(np.ones(s), F16) for s in ((40, 24), (24, 9), (40, 9)))
     for g in lt().linear_backward(F, X, place(np.zeros((40, 9)), F16), pre=z, activation="gelu"):
         assert not host(g).any()
+
+
+def test_the_factor_follows_the_gradients():
+    """Captured once and replayed with gradients of other sizes, eager work between
+    the replays: the factor is that of the call's own dO, on any stream."""
+    r = rng(24)
+    kn, ci, t = 264, 136, 40
+    F, X, z = (place(r.standard_normal(s), F16) for s in ((kn, ci), (ci, t), (kn, t)))
+    d = r.standard_normal((kn, t))
+    dO = place(d, F16)
+
+    def call():
+        return lt().linear_backward(F, X, dO, pre=z, activation="gelu")
+
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = call()
+    side = torch.cuda.Stream()
+    for size in (2.0 ** -20, 8.0, 2.0 ** -8, 2.0 ** -20):
+        dO.copy_(torch.from_numpy(d * size).to(F16))
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [v.clone() for v in got]
+        eager = call()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = call()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        h = [host(v) for v in (F, X, dO, z)]
+        for a, b, c, want, bound, name in zip(replayed, eager, other, lt64.backward(*h, "gelu"), bounds(*h, "gelu"), ("dX", "dF", "dbias")):
+            assert torch.equal(a, b) and torch.equal(b, c), (size, name)
+            near(a, want, bound, name)
