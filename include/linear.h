@@ -44,8 +44,8 @@
  * at F[c + ldf k]).  Any leading dimension and any address that the type
  * allows are taken; operands whose addresses, leading dimensions or contiguous
  * extents are not multiples of 16 bytes cost narrower loads (fp32), a padded copy
- * (16-bit types) or, up to 64 tokens, loads through registers; so do lines of
- * 2^22 fp32 or 2^23 16-bit values and more.
+ * (16-bit types) or, up to 64 tokens, loads through registers; lines of 2^22 fp32
+ * or 2^23 16-bit values and more always go through registers.
  *
  * Rules (as in ltlt.h): pointers are DEVICE pointers of the current HIP device
  * unless marked HOST; calls are stream-ordered and asynchronous; the caller
@@ -124,9 +124,10 @@ int64_t convgemm_linear_backward_workspace(int dtype, int64_t kn, int64_t ci, in
                                            int aligned);
 
 /* dX, dF and dbias from dO; each of the three may be NULL and is then not
- * computed (the bytes that the query names are enough all the same).  F may be NULL where dX is, X where dF is.  Z is the pre-activation
- * that convgemm_linear wrote; it is not looked at where act is LINEAR_ACT_NONE.
- * dF has F's order; its leading dimension is lddf. */
+ * computed (the bytes that the query names are enough all the same).  F may be
+ * NULL where dX is, X where dF is.  Z is the pre-activation that convgemm_linear
+ * wrote; it is not looked at where act is LINEAR_ACT_NONE.  dF has F's order; its
+ * leading dimension is lddf. */
 int convgemm_linear_backward(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order, int64_t ldf,
                              const void* X, int64_t ldx, const void* dO, int64_t lddo, const void* Z, int64_t ldz,
                              int act, void* dX, int64_t lddx, void* dF, int64_t lddf, void* dbias, void* workspace,

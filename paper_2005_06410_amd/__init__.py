@@ -657,7 +657,9 @@ def linear_backward(F, X, dO, pre=None, activation: str = "none", needs=(True, T
     (``convgemm_linear_backward``); the residual's gradient is dO itself.
 
     ``pre`` is the Z that ``linear(..., keep_pre=True)`` returned; without an
-    activation it is not needed.  dX is stored like X, dF in F's order.
+    activation it is not needed.  dX is stored like X, dF in F's order.  Between
+    the two products dO act'(Z) is rounded to the layer's type once (fp16: times a
+    power of two, so that its range does not matter).
     ``needs`` leaves out what is not wanted (None is returned in its place)."""
     ci, t, ldx, dtype, code, dev = _layer_input(X)
     kn, order, ldf = _weights(F, ci, dtype, dev)
