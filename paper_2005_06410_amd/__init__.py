@@ -50,6 +50,10 @@ __all__ = [
     "linear_choice",
     "grad_norm",
     "clip_grad_norm",
+    "linear_cross_entropy",
+    "linear_cross_entropy_backward",
+    "linear_distill",
+    "linear_distill_backward",
     "LtltError",
     "F64",
     "F32",
@@ -60,6 +64,14 @@ F64, F32, C128, C64 = 0, 1, 2, 3
 BATCHED_MAX_N = 64
 _lock = threading.Lock()
 _lib = None
+
+# include/loss.h: arguments that several calls share
+_LAYER = ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64]
+          + [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p])
+_LABELS = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64]
+_TEACHER = [ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64] * 2 + [ctypes.c_double]
+_GRADIENTS = ([ctypes.c_void_p] * 2 + [ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int64] * 2 + [ctypes.c_void_p] * 2
+              + [ctypes.c_int64, ctypes.c_void_p])
 
 _SYMBOLS = {
     "ltlt_factor": ([ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p,
@@ -111,6 +123,13 @@ _SYMBOLS = {
     "convgemm_grad_norm": ([ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
     "convgemm_grad_clip": ([ctypes.c_int] + [ctypes.c_void_p] * 4 + [ctypes.c_double] + [ctypes.c_void_p] * 2
                            + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    # include/loss.h
+    "convgemm_linear_loss_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 3, ctypes.c_int64),
+    "convgemm_linear_loss_backward_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_int] * 3, ctypes.c_int64),
+    "convgemm_linear_cross_entropy": (_LAYER + _LABELS + [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    "convgemm_linear_distill": (_LAYER + _TEACHER + [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    "convgemm_linear_cross_entropy_backward": (_LAYER + _LABELS + _GRADIENTS, ctypes.c_int),
+    "convgemm_linear_distill_backward": (_LAYER + _TEACHER + _GRADIENTS, ctypes.c_int),
 }
 
 
@@ -688,6 +707,170 @@ def linear_backward(F, X, dO, pre=None, activation: str = "none", needs=(True, T
     _launch("convgemm_linear_backward", dev, code, kn, ci, t, F.data_ptr(), order, ldf, X.data_ptr(), ldx, dO.data_ptr(),
             lddo, zp, ldz, act, xp, max(ci, 1), fp, max(ci if order else kn, 1), bp, ws.data_ptr() if need else 0, need)
     return dX, dF, db
+
+
+def _loss_layer(F, X, bias):
+    """What the losses ask of the layer whose outputs they take: (kn, ci, t, dtype's
+    code, GPU index, F's order, the C arguments up to bias, whether aligned)."""
+    ci, t, ldx, dtype, code, dev = _layer_input(X)
+    kn, order, ldf = _weights(F, ci, dtype, dev)
+    bp = 0
+    if bias is not None:
+        if bias.shape != (kn,) or (kn > 1 and bias.stride(0) != 1):
+            raise ValueError(f"bias must be a contiguous tensor of {kn} values")
+        if bias.dtype != dtype:
+            raise TypeError("bias must have X's dtype")
+        if bias.get_device() != dev:
+            raise ValueError("all tensor arguments must be on the same GPU")
+        bp = bias.data_ptr()
+    fp, xp = F.data_ptr(), X.data_ptr()
+    return kn, ci, t, code, dev, order, (code, kn, ci, t, fp, order, ldf, xp, ldx, bp), _aligned(code, ldf | ldx, fp | xp)
+
+
+def _index_code(v, name: str) -> int:
+    torch = _torch()
+    if v.dtype == torch.int64:
+        return 2
+    if v.dtype == torch.int32:
+        return 1
+    raise TypeError(f"{name} must be int64 or int32")
+
+
+def _per_token(v, t: int, name: str, dev: int):
+    if v.shape != (t,) or (t > 1 and v.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous tensor of {t} values")
+    if v.get_device() != dev:
+        raise ValueError("all tensor arguments must be on the same GPU")
+
+
+def _label_args(labels, t: int, ignore_index: int, dev: int):
+    code = _index_code(labels, "labels")
+    _per_token(labels, t, "labels", dev)
+    return 0, (labels.data_ptr(), code, int(ignore_index))
+
+
+def _teacher_args(top, index, t: int, temperature: float, dev: int):
+    if top.dim() != 2 or not 1 <= top.shape[0] <= 1024:
+        raise ValueError("top must be (k, t), k from 1 to 1024")
+    k = top.shape[0]
+    ttype = _layer_dtype(top.dtype)
+    ldtop = _columns(top, k, t, "top", top.dtype, dev)
+    itype = _index_code(index, "index")
+    ldi = _columns(index, k, t, "index", index.dtype, dev)
+    temperature = float(temperature)
+    if not 0 < temperature < 1e18 or not 1 / temperature < 1e18:
+        raise ValueError("temperature must be positive and finite")
+    return k, (k, top.data_ptr(), ttype, ldtop, index.data_ptr(), itype, ldi, temperature)
+
+
+def _loss_forward(fn: str, layer, k: int, target, X):
+    kn, ci, t, code, dev, order, args, aligned = layer
+    loss, lse = X.new_empty(t, dtype=_torch().float32), X.new_empty(t, dtype=_torch().float32)
+    need = _scratch_bytes("convgemm_linear_loss_workspace", dev, code, kn, ci, t, order, k, aligned)
+    ws = _scratch(need, X) if need else None
+    _launch(fn, dev, *args, *target, loss.data_ptr(), lse.data_ptr(), ws.data_ptr() if need else 0, need)
+    return loss, lse
+
+
+def _loss_backward(fn: str, layer, k: int, target, X, lse, dloss, needs):
+    kn, ci, t, code, dev, order, args, aligned = layer
+    torch = _torch()
+    if lse.dtype != torch.float32 or dloss.dtype != torch.float32:
+        raise TypeError("lse and dloss must be float32")
+    _per_token(lse, t, "lse", dev)
+    if dloss.dim() == 0:
+        if dloss.get_device() != dev:
+            raise ValueError("all tensor arguments must be on the same GPU")
+        ginc = 0
+    elif dloss.shape == (t,) and t > 1 and dloss.stride(0) == 0 and dloss.get_device() == dev:
+        ginc = 0
+    else:
+        _per_token(dloss, t, "dloss", dev)
+        ginc = 1
+    dX = dF = db = None
+    xp = fp = bp = 0
+    if needs[0]:
+        dX = X.new_empty_strided((ci, t), (1, max(ci, 1)))
+        xp = dX.data_ptr()
+    if needs[1]:
+        dF = X.new_empty_strided((kn, ci), (max(ci, 1), 1) if order else (1, max(kn, 1)))
+        fp = dF.data_ptr()
+    if needs[2]:
+        db = X.new_empty(kn)
+        bp = db.data_ptr()
+    if not (needs[0] or needs[1] or needs[2]):
+        return dX, dF, db
+    need = _scratch_bytes("convgemm_linear_loss_backward_workspace", dev, code, kn, ci, t, order, k, aligned)
+    ws = _scratch(need, X)
+    _launch(fn, dev, *args, *target, lse.data_ptr(), dloss.data_ptr(), ginc, xp, max(ci, 1), fp, max(ci if order else kn, 1), bp,
+            ws.data_ptr(), need)
+    return dX, dF, db
+
+
+def linear_cross_entropy(F, X, labels, bias=None, ignore_index: int = -100):
+    """Softmax cross entropy of the layer Z = F X + bias over its kn classes, without Z
+    in memory (``convgemm_linear_cross_entropy``).
+
+    F, X and ``bias`` are ``linear``'s: F (kn, ci) with either index fastest, X (ci, t)
+    stored leftmost index fastest, float32, bfloat16 or float16.  ``labels``: t classes,
+    int64 or int32.  Returns (loss, lse), t float32 values each:
+
+        lse[n] = log sum_m exp(Z[m, n]),    loss[n] = lse[n] - Z[labels[n], n],
+
+    and loss 0 where labels[n] is ``ignore_index``; a label outside the classes gives
+    NaN.  ``lse`` is what ``linear_cross_entropy_backward`` takes; -loss is the label's
+    log probability.  A bias of -infinity takes a class out.  Nothing is recorded for
+    torch's automatic differentiation."""
+    layer = _loss_layer(F, X, bias)
+    k, target = _label_args(labels, layer[2], ignore_index, layer[4])
+    return _loss_forward("convgemm_linear_cross_entropy", layer, k, target, X)
+
+
+def linear_cross_entropy_backward(F, X, labels, lse, dloss, bias=None, ignore_index: int = -100, needs=(True, True, True)):
+    """(dX, dF, dbias) of ``linear_cross_entropy`` from ``dloss`` = dL/dloss, t float32
+    values on the GPU or a single one for all tokens (``convgemm_linear_cross_entropy_backward``):
+
+        dZ[m, n] = dloss[n] (exp(Z[m, n] - lse[n]) - [m == labels[n]]),
+        dX = F^T dZ,    dF = dZ X^T,    dbias = dZ 1.
+
+    Z is computed again, a piece of 8192 classes or more at a time; a piece's dZ is
+    rounded to the layer's type once (fp16: times a power of two), dX is summed over the
+    pieces in float32.  Ignored tokens, and tokens with dloss = 0, add nothing whatever
+    their X holds.  dX is stored like X, dF in F's order; ``needs`` leaves out what is
+    not wanted (None is returned in its place)."""
+    layer = _loss_layer(F, X, bias)
+    k, target = _label_args(labels, layer[2], ignore_index, layer[4])
+    return _loss_backward("convgemm_linear_cross_entropy_backward", layer, k, target, X, lse, dloss, needs)
+
+
+def linear_distill(F, X, top, index, bias=None, temperature: float = 1.0):
+    """Distillation of the layer Z = F X + bias from a teacher's k largest logits of each
+    token, without Z in memory (``convgemm_linear_distill``).
+
+    ``top`` (k, t): the logits, float32, bfloat16 or float16; ``index`` (k, t): their
+    classes, int64 or int32; both stored leftmost index fastest (``torch.topk(...)`` of
+    row-major logits, transposed), in any order, k up to 1024.  With q the softmax of
+    top / T over the k entries and p that of Z / T over all classes, returns
+    (loss, lse), t float32 values each:
+
+        loss[n] = T^2 sum_j q[j, n] (log q[j, n] - log p[index[j, n], n]),
+
+    lse the logarithm of sum_m exp(Z[m, n] / T).  Entries with a negative index or the
+    logit -infinity do not count (tokens may have fewer than k); a token without any has
+    loss 0.  An index beyond the classes gives NaN.  Equal classes of a token add up."""
+    layer = _loss_layer(F, X, bias)
+    k, target = _teacher_args(top, index, layer[2], temperature, layer[4])
+    return _loss_forward("convgemm_linear_distill", layer, k, target, X)
+
+
+def linear_distill_backward(F, X, top, index, lse, dloss, bias=None, temperature: float = 1.0, needs=(True, True, True)):
+    """(dX, dF, dbias) of ``linear_distill`` from ``dloss`` (``convgemm_linear_distill_backward``):
+    as ``linear_cross_entropy_backward``, with
+
+        dZ[m, n] = dloss[n] T (p[m, n] - sum of q[j, n] with index[j, n] == m)."""
+    layer = _loss_layer(F, X, bias)
+    k, target = _teacher_args(top, index, layer[2], temperature, layer[4])
+    return _loss_backward("convgemm_linear_distill_backward", layer, k, target, X, lse, dloss, needs)
 
 
 def _dense(t) -> bool:

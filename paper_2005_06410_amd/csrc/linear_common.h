@@ -192,7 +192,8 @@ struct Product {
   Lines a, b;             // the operands' lines, as the workspace was sized for
   int splits;             // workgroups that share a tile's contraction
   int mtiles, ntiles;
-  float* part;            // splits > 1: [splits][N][M] partial products
+  float* part;            // [splits][N][M] partial products, or nullptr where the epilogue follows (splits = 1)
+  bool add;               // the partial products are added to what `part` holds
   Epilogue e;
 };
 
@@ -267,6 +268,14 @@ int64_t product_workspace(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int
 
 // p.arows, aK, brows, bK: the extents as loaded, or 0 where they are M, N and K.
 hipError_t launch_product(int dtype, bool a_kc, bool b_kc, Product p, void* workspace, hipStream_t s);
+
+// A contraction whose operands come piece by piece: the partial products of one
+// piece, written to p.part or (p.add) added to it, p.splits of them (at least
+// product_splits() of the largest piece); then what launch_product() does with their
+// sum.  The operands' lines are kDirect, or kFar even in a padded copy.
+int product_splits(int dtype, bool a_kc, bool b_kc, Lines a, Lines b, int64_t M, int64_t N, int64_t K);
+hipError_t launch_product_part(int dtype, bool a_kc, bool b_kc, Product p, hipStream_t s);
+hipError_t launch_product_join(int dtype, const Product& p, hipStream_t s);
 
 // Argument checks of the C ABI.
 constexpr int64_t kSizeLimit = 1ll << 24;

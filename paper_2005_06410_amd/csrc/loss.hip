@@ -1,0 +1,378 @@
+// Losses over a layer's outputs, forward: Z = F X + bias is never written; each wave
+// ends its tile with the maximum and the sum of exponentials of its rows, and with the
+// targets' logits; a second launch joins the waves' parts of a column.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "loss_common.h"
+
+namespace linear {
+namespace {
+
+// Where maxima are infinite, exponentials are taken without one: exp(+inf) = inf and
+// exp(-inf) = 0 are then what the formula says, and nothing is inf - inf.
+__device__ inline float base_of(float top) { return fabsf(top) < INFINITY ? top : 0.0f; }
+
+// Ends a wave's tile with its columns' statistics.
+struct StatsEnd {
+  using P = LossProduct;
+  template <class T, int VA, int VB, bool STREAM, int WM, int WN>
+  static __device__ void tile(const P& p, int, int m0, int n0, int lane, char*, f4 (&acc)[WM][WN]) {
+    static_assert(VB == 1, "X's contraction is contiguous");
+    constexpr int ROWS = 16 * WM;
+    if (m0 >= p.M) return;
+    const int q = lane >> 4, l16 = lane & 15;
+    const bool edge = m0 + ROWS > p.M;
+    const T* b = static_cast<const T*>(p.bias);
+    float bias[WM][4];
+    if (b) {
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bias[i][r] = p.scale * (float)b[min(m0 + row_of<VA>(i, r, q), p.M - 1)];
+    } else {
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bias[i][r] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+      const int n = n0 + 16 * j + l16;
+      int lo, hi;
+      entries_of(p.y, n, n < p.N, p.row0 + m0, ROWS, lo, hi);
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float z = acc[i][j][r] * p.scale + bias[i][r];
+          if (edge && m0 + row_of<VA>(i, r, q) >= p.M) z = -INFINITY;
+          acc[i][j][r] = z;
+          top = fmaxf(top, z);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float base = base_of(top);
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += exp_of<T>(acc[i][j][r] - base);
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (q == 0 && n < p.N) p.sums[(int64_t)(m0 / ROWS) * p.N + n] = float2{top, sum};
+      for (int e = lo; e < hi; ++e) {
+        const int64_t rel = entry_row(p.y, n, e, p.row0 + m0);
+        if (rel < 0 || rel >= ROWS) continue;
+        float z = 0.0f;
+        bool mine = false;
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool is = row_of<VA>(i, r, q) == (int)rel;
+            z = is ? acc[i][j][r] : z;
+            mine |= is;
+          }
+        if (mine) p.at[p.y.label ? (int64_t)n : (int64_t)n * p.y.k + e] = z;
+      }
+    }
+  }
+};
+
+// Joins the parts of C columns a workgroup, 256 / C lanes for each, in a fixed order:
+//   lse = base + log sum exp(top_r - base) sum_r,
+// then the loss.  Bound by latency: what it reads is an eighth or less of a percent of
+// the product's operands.
+template <int C>
+__global__ __launch_bounds__(256) void join_loss_kernel(int parts, int N, int64_t kn, const float2* __restrict__ sums,
+                                                        const float* __restrict__ at, Targets y, float temperature2,
+                                                        float* __restrict__ loss, float* __restrict__ lse) {
+  constexpr int LANES = 256 / C;
+  __shared__ float sh[LANES][C];
+  const int c = threadIdx.x % C, x = threadIdx.x / C, n = blockIdx.x * C + c;
+  const bool there = n < N;
+  auto over = [&](float v, auto f) {
+    sh[x][c] = v;
+    __syncthreads();
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) {
+      if (x < d) sh[x][c] = f(sh[x][c], sh[x + d][c]);
+      __syncthreads();
+    }
+    v = sh[0][c];
+    __syncthreads();
+    return v;
+  };
+  const float2* s = sums + n;
+  float top = -INFINITY;
+  if (there) {
+#pragma unroll 8
+    for (int r = x; r < parts; r += LANES) top = fmaxf(top, s[(int64_t)r * N].x);
+  }
+  top = over(top, [](float a, float b) { return fmaxf(a, b); });
+  const float base = base_of(top);
+  float sum = 0.0f;
+  if (there) {
+#pragma unroll 8
+    for (int r = x; r < parts; r += LANES) {
+      const float2 v = s[(int64_t)r * N];
+      // a part of -inf alone has the sum 0 (or NaN), whatever it is taken relative to
+      sum += v.x == -INFINITY ? v.y : v.y * expf(base_of(v.x) - base);
+    }
+  }
+  sum = over(sum, [](float a, float b) { return a + b; });
+  const float l = base + logf(sum);
+  if (y.label) {
+    if (!there || x > 0) return;
+    const int64_t label = label_of(y, n);
+    lse[n] = l;
+    loss[n] = label == y.ignore ? 0.0f : label >= 0 && label < kn ? l - at[n] : NAN;
+    return;
+  }
+  const int count = there ? y.count[n] : 0;
+  float v = 0.0f;
+  for (int e = x; e < count; e += LANES) {
+    const int64_t i = (int64_t)n * y.k + e;
+    const float w = y.weight[i];
+    v += w == 0.0f ? 0.0f : w * (logf(w) - (at[i] - l));
+  }
+  v = over(v, [](float a, float b) { return a + b; });
+  if (!there || x > 0) return;
+  lse[n] = l;
+  loss[n] = count < 0 ? NAN : count == 0 ? 0.0f : temperature2 * v;
+}
+
+// The teacher of one column, by one wave: its entries sorted by class (a bitonic
+// network over class and place, so that equal classes keep their order), the weights
+// q in fp32, and the first entry of every 128 classes.
+template <class TT>
+__global__ __launch_bounds__(64) void list_kernel(int64_t kn, int k, int size, const TT* __restrict__ top, int64_t ldtop,
+                                                  const void* __restrict__ index, int64_t ldi, int wide, float scale, int bins,
+                                                  int* __restrict__ sorted, float* __restrict__ weight,
+                                                  uint16_t* __restrict__ bin, int* __restrict__ count) {
+  __shared__ uint64_t key[LOSS_MAX_K];
+  __shared__ float value[LOSS_MAX_K];
+  const int64_t n = blockIdx.x;
+  const int lane = threadIdx.x;
+  float best = -INFINITY;
+  bool bad = false;
+  int valid = 0;
+  for (int e = lane; e < size; e += 64) {
+    uint64_t at = ~0ull;
+    float v = -INFINITY;
+    if (e < k) {
+      const int64_t i = wide ? static_cast<const int64_t*>(index)[n * ldi + e] : (int64_t)static_cast<const int*>(index)[n * ldi + e];
+      v = (float)top[n * ldtop + e];
+      if (i >= 0 && v != -INFINITY) {
+        ++valid;
+        bad |= i >= kn;
+        at = (uint64_t)min(i, kn) << 16 | (uint64_t)e;
+        best = fmaxf(best, v);
+      }
+    }
+    key[e] = at;
+    value[e] = v;
+  }
+  for (int d = 32; d > 0; d >>= 1) {
+    best = fmaxf(best, __shfl_xor(best, d));
+    valid += __shfl_xor(valid, d);
+  }
+  bad = __any(bad);
+  __syncthreads();
+  for (int outer = 2; outer <= size; outer <<= 1)
+    for (int d = outer >> 1; d > 0; d >>= 1) {
+      for (int i = lane; i < size / 2; i += 64) {
+        const int a = 2 * i - (i & (d - 1)), b = a + d;
+        const uint64_t x = key[a], y = key[b];
+        if ((x > y) == ((a & outer) == 0)) key[a] = y, key[b] = x;
+      }
+      __syncthreads();
+    }
+  float sum = 0.0f;
+  for (int e = lane; e < valid; e += 64) sum += expf((value[key[e] & 0xffff] - best) * scale);
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  for (int e = lane; e < valid; e += 64) {
+    sorted[n * k + e] = (int)(key[e] >> 16);
+    weight[n * k + e] = expf((value[key[e] & 0xffff] - best) * scale) / sum;
+  }
+  uint16_t* out = bin + n * (bins + 1);
+  for (int b = lane; b <= bins; b += 64) {
+    int lo = 0, hi = valid;                   // the first entry of class 128 b or later
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if ((int64_t)(key[mid] >> 16) < (int64_t)b * kBin)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    out[b] = (uint16_t)lo;
+  }
+  if (lane == 0) count[n] = bad ? -1 : valid;
+}
+
+struct Forward {
+  LossPlan plan;
+  int64_t copies, sums, at, lists, bytes;   // byte offsets
+  int parts;
+};
+
+Forward forward_layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int k, Lines f, Lines x) {
+  Forward w{};
+  w.plan = loss_plan(dtype, f_order == 1, f, x, kn, t, ci);
+  w.parts = (int)ceil_div(kn, w.plan.rows);
+  if (w.plan.route.copy_a) w.sums += up256(copy_values(dtype, f_order == 1, kn, ci) * type_size(dtype));
+  if (w.plan.route.copy_b) w.sums += up256(copy_values(dtype, true, t, ci) * type_size(dtype));
+  w.at = w.sums + up256((int64_t)w.parts * t * 8);
+  w.lists = w.at + up256(t * std::max(k, 1) * 4);
+  w.bytes = w.lists + (k ? list_bytes(kn, t, k) : 0);
+  return w;
+}
+
+int loss_forward(const LossCall& c, float* loss, float* lse, char* ws, hipStream_t s) {
+  if (c.t == 0) return LINEAR_OK;
+  const Lines f = lines_of(c.dtype, c.F, c.ldf, c.f_order ? c.ci : c.kn), x = lines_of(c.dtype, c.X, c.ldx, c.ci);
+  const Forward w = forward_layout(c.dtype, c.kn, c.ci, c.t, c.f_order, c.k, f, x);
+  LossProduct p{};
+  p.A = c.F;
+  p.lda = c.ldf;
+  p.B = c.X;
+  p.ldb = c.ldx;
+  p.M = (int)c.kn;
+  p.N = (int)c.t;
+  p.K = (int)c.ci;
+  p.a = f;
+  p.b = x;
+  p.bias = c.bias;
+  p.scale = (float)(1.0 / c.temperature);
+  p.sums = reinterpret_cast<float2*>(ws + w.sums);
+  p.at = reinterpret_cast<float*>(ws + w.at);
+  hipError_t e = hipSuccess;
+  if (c.k)
+    e = launch_lists(c, ws + w.lists, p.y, s);
+  else
+    p.y = Targets{c.labels, c.itype == LOSS_I64, c.ignore, nullptr, nullptr, nullptr, nullptr, 0, 0};
+  if (e == hipSuccess && c.kn > 0) e = launch_loss<StatsEnd>(c.dtype, c.f_order == 1, p, ws, s);
+  if (e != hipSuccess) return LINEAR_ERR_HIP_BASE - (int)e;
+  const float t2 = (float)(c.temperature * c.temperature);
+  if (c.t >= 256)
+    join_loss_kernel<16><<<dim3((unsigned)((c.t + 15) / 16)), 256, 0, s>>>(w.parts, p.N, c.kn, p.sums, p.at, p.y, t2, loss, lse);
+  else
+    join_loss_kernel<1><<<dim3((unsigned)c.t), 256, 0, s>>>(w.parts, p.N, c.kn, p.sums, p.at, p.y, t2, loss, lse);
+  e = hipGetLastError();
+  return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
+}
+
+int64_t need_of(const LossCall& c) {
+  return forward_layout(c.dtype, c.kn, c.ci, c.t, c.f_order, c.k, lines_of(c.dtype, c.F, c.ldf, c.f_order ? c.ci : c.kn),
+                        lines_of(c.dtype, c.X, c.ldx, c.ci)).bytes;
+}
+
+}  // namespace
+
+int check_loss_layer(const LossCall& c) {
+  if (int e = check_sizes(c.dtype, c.kn, c.ci, c.t)) return e;
+  const bool work = c.kn > 0 && c.ci > 0 && c.t > 0;
+  if (!c.F && work) return -5;
+  if (c.f_order != 0 && c.f_order != 1) return -6;
+  if (bad_ld(c.ldf, c.f_order ? c.ci : c.kn)) return -7;
+  if (!c.X && work) return -8;
+  if (bad_ld(c.ldx, c.ci)) return -9;
+  return 0;
+}
+
+int check_teacher(const LossCall& c) {
+  if (c.k < 1 || c.k > LOSS_MAX_K || c.t * c.k >= kElemLimit) return -11;
+  if (!c.top && c.t > 0) return -12;
+  if (!is_type(c.ttype)) return -13;
+  if (bad_ld(c.ldtop, c.k)) return -14;
+  if (!c.index && c.t > 0) return -15;
+  if (c.itype != LOSS_I32 && c.itype != LOSS_I64) return -16;
+  if (bad_ld(c.ldi, c.k)) return -17;
+  if (!(c.temperature > 0) || !std::isfinite((float)c.temperature) || !std::isfinite((float)(1.0 / c.temperature)) ||
+      !std::isfinite((float)(c.temperature * c.temperature)))
+    return -18;
+  return 0;
+}
+
+int64_t list_bytes(int64_t kn, int64_t t, int k) {
+  const int64_t bins = ceil_div(kn, kBin);
+  return 2 * up256(t * k * 4) + up256(t * (bins + 1) * 2) + up256(t * 4);
+}
+
+hipError_t launch_lists(const LossCall& c, char* ws, Targets& y, hipStream_t s) {
+  const int64_t bins = ceil_div(c.kn, kBin);
+  int* sorted = reinterpret_cast<int*>(ws);
+  ws += up256(c.t * c.k * 4);
+  float* weight = reinterpret_cast<float*>(ws);
+  ws += up256(c.t * c.k * 4);
+  uint16_t* bin = reinterpret_cast<uint16_t*>(ws);
+  ws += up256(c.t * (bins + 1) * 2);
+  int* count = reinterpret_cast<int*>(ws);
+  y = Targets{nullptr, 0, 0, sorted, weight, bin, count, c.k, (int)bins};
+  int size = 2;
+  while (size < c.k) size *= 2;
+  auto launch = [&](auto* top) {
+    list_kernel<<<dim3((unsigned)c.t), 64, 0, s>>>(c.kn, c.k, size, top, c.ldtop, c.index, c.ldi, c.itype == LOSS_I64,
+                                                   (float)(1.0 / c.temperature), (int)bins, sorted, weight, bin, count);
+    return hipGetLastError();
+  };
+  switch (c.ttype) {
+    case LINEAR_F32: return launch(static_cast<const float*>(c.top));
+    case LINEAR_BF16: return launch(static_cast<const bf16*>(c.top));
+    default: return launch(static_cast<const f16*>(c.top));
+  }
+}
+
+}  // namespace linear
+
+extern "C" int64_t convgemm_linear_loss_workspace(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int k, int aligned) {
+  using namespace linear;
+  if (int e = check_sizes(dtype, kn, ci, t)) return e;
+  if (f_order != 0 && f_order != 1) return -5;
+  if (k < 0 || k > LOSS_MAX_K || t * k >= kElemLimit) return -6;
+  if (t == 0) return 0;
+  if (aligned)
+    return forward_layout(dtype, kn, ci, t, f_order, k, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci)).bytes;
+  int64_t most = 0;
+  for (Lines f : kAnyLines)
+    for (Lines x : kAnyLines) most = std::max(most, forward_layout(dtype, kn, ci, t, f_order, k, f, x).bytes);
+  return most;
+}
+
+extern "C" int convgemm_linear_cross_entropy(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order,
+                                             int64_t ldf, const void* X, int64_t ldx, const void* bias, const void* labels,
+                                             int itype, int64_t ignore, float* loss, float* lse, void* workspace,
+                                             int64_t workspace_bytes, hipStream_t stream) {
+  using namespace linear;
+  const LossCall c{dtype, kn, ci, t, F, f_order, ldf, X, ldx, bias, labels, ignore, 0, nullptr, 0, 0, nullptr, 0, 1.0, itype};
+  if (int e = check_loss_layer(c)) return e;
+  if (!labels && t > 0) return -11;
+  if (itype != LOSS_I32 && itype != LOSS_I64) return -12;
+  if (!loss && t > 0) return -14;
+  if (!lse && t > 0) return -15;
+  if (t == 0) return LINEAR_OK;
+  if (!workspace || ((uintptr_t)workspace & 15)) return -16;
+  if (workspace_bytes < need_of(c)) return -17;
+  return loss_forward(c, loss, lse, static_cast<char*>(workspace), stream);
+}
+
+extern "C" int convgemm_linear_distill(int dtype, int64_t kn, int64_t ci, int64_t t, const void* F, int f_order, int64_t ldf,
+                                       const void* X, int64_t ldx, const void* bias, int k, const void* top, int ttype,
+                                       int64_t ldtop, const void* index, int itype, int64_t ldi, double temperature,
+                                       float* loss, float* lse, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  using namespace linear;
+  const LossCall c{dtype, kn, ci, t, F, f_order, ldf, X, ldx, bias, nullptr, 0, k, top, ttype, ldtop, index, ldi, temperature, itype};
+  if (int e = check_loss_layer(c)) return e;
+  if (int e = check_teacher(c)) return e;
+  if (!loss && t > 0) return -19;
+  if (!lse && t > 0) return -20;
+  if (t == 0) return LINEAR_OK;
+  if (!workspace || ((uintptr_t)workspace & 15)) return -21;
+  if (workspace_bytes < need_of(c)) return -22;
+  return loss_forward(c, loss, lse, static_cast<char*>(workspace), stream);
+}

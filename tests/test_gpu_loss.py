@@ -1,0 +1,435 @@
+"""Losses over a layer's outputs against their 64-bit forms: cross entropy from labels
+and distillation from a teacher's largest logits, with their gradients, at the sizes,
+orders, masks and columns where they can go wrong."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import loss_truths as truth
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+IGNORE = -100
+
+
+def lt():
+    import paper_2005_06410_amd as m
+    return m
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def stored(g, rows, cols, dtype, scale=1.0, order=0, pad=0, shift=0):
+    """(rows, cols) normal values: the first (order 0) or the second index fastest,
+    `pad` values between lines, `shift` values into its buffer."""
+    lines, length = (cols, rows) if order == 0 else (rows, cols)
+    flat = torch.full((shift + lines * (length + pad) + 8,), 7.0, dtype=dtype, device="cuda")
+    view = flat[shift:shift + lines * (length + pad)].view(lines, length + pad)[:, :length]
+    view.copy_(torch.randn(lines, length, generator=g, device="cuda") * scale)
+    return view.t() if order == 0 else view
+
+
+def layer(g, kn, ci, t, dtype, order, bias=True, pad=0, shift=0, spread=2.0):
+    F = stored(g, kn, ci, dtype, spread * max(ci, 1) ** -0.5, order, pad, shift)
+    X = stored(g, ci, t, dtype, 1.0, 0, pad, shift)
+    return F, X, (torch.randn(kn, generator=g, device="cuda") * 0.5).to(dtype) if bias else None
+
+
+def labels_of(g, kn, t, dtype=torch.int64, ignored=0.2):
+    y = torch.randint(0, kn, (t,), generator=g, device="cuda")
+    return torch.where(torch.rand(t, generator=g, device="cuda") < ignored, IGNORE, y).to(dtype)
+
+
+def teacher_of(g, kn, t, k, dtype, itype=torch.int64):
+    """k logits a column, some entries left out, some classes twice, one column empty."""
+    top = (torch.randn(t, k, generator=g, device="cuda") * 2).to(dtype)
+    index = torch.randint(0, kn, (t, k), generator=g, device="cuda")
+    if k > 2:
+        index[:, 1] = index[:, 0]
+        index[::3, 2] = -1
+        top[1::4, 1] = -torch.inf
+    if t > 2:
+        index[2] = -1
+    return top.t(), index.to(itype).t()
+
+
+def forward(F, X, bias, case):
+    if "labels" in case:
+        return lt().linear_cross_entropy(F, X, case["labels"], bias=bias, ignore_index=case["ignore"])
+    return lt().linear_distill(F, X, case["top"], case["index"], bias=bias, temperature=case["temperature"])
+
+
+def backward(F, X, bias, case, lse, g, **kw):
+    if "labels" in case:
+        return lt().linear_cross_entropy_backward(F, X, case["labels"], lse, g, bias=bias, ignore_index=case["ignore"], **kw)
+    return lt().linear_distill_backward(F, X, case["top"], case["index"], lse, g, bias=bias, temperature=case["temperature"], **kw)
+
+
+def within(got, want, bound, what):
+    got = got.double()
+    off = (got - want).abs()
+    bad = ~(off <= bound) & ~((got == want) | (got.isnan() & want.isnan()))
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, the worst {float((off / bound)[bad].max()):.3g} times its bound"
+
+
+def check(F, X, bias, case, g, needs=(True, True, True)):
+    loss, lse = forward(F, X, bias, case)
+    for got, want, bound, what in zip((loss, lse), truth.forward(F, X, bias, case), truth.forward_bound(F, X, bias, case), ("loss", "lse")):
+        within(got, want, bound, what)
+    grads = backward(F, X, bias, case, lse, g, needs=needs)
+    for got, want, bound, what in zip(grads, truth.backward(F, X, bias, case, g), truth.backward_bound(F, X, bias, case, g, X.dtype),
+                                      ("dX", "dF", "dbias")):
+        if got is not None:
+            assert got.dtype == X.dtype and got.shape == want.shape
+            within(got, want, bound, what)
+    return loss, lse, grads
+
+
+def gradient_of(g, t):
+    return torch.randn(t, generator=g, device="cuda") / t + 1.0 / t
+
+
+# one of everything; whole tiles; nothing whole; few and many columns of each kind of kernel
+SIZES = [(1, 1, 1), (2, 1, 3), (5, 3, 2), (64, 64, 1), (1000, 64, 80), (1001, 515, 77), (257, 40, 1), (130, 8, 300), (513, 100, 65),
+         (3000, 33, 17), (20000, 72, 40), (4096, 512, 512), (1536, 256, 2048), (127, 4096, 33), (2048, 1000, 5), (40000, 64, 9)]
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kn,ci,t", SIZES)
+def test_cross_entropy(kn, ci, t, dtype, order):
+    g = gen(kn + t)
+    F, X, b = layer(g, kn, ci, t, dtype, order, bias=order == 0)
+    check(F, X, b, {"labels": labels_of(g, kn, t, torch.int64 if order else torch.int32), "ignore": IGNORE}, gradient_of(g, t))
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kn,ci,t,k", [(1, 1, 1, 1), (7, 3, 4, 3), (1000, 64, 80, 5), (1001, 515, 77, 64), (257, 40, 1, 128), (4096, 512, 512, 17),
+                                       (3000, 33, 17, 1000), (20000, 72, 40, 1024), (1536, 256, 2048, 8)])
+def test_distill(kn, ci, t, k, dtype, order):
+    g = gen(kn + t + k)
+    F, X, b = layer(g, kn, ci, t, dtype, order, bias=order == 1)
+    top, index = teacher_of(g, kn, t, k, dtype if order else torch.float32, torch.int64 if order else torch.int32)
+    check(F, X, b, {"top": top, "index": index, "temperature": 2.0 if order else 1.0}, gradient_of(g, t))
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (0, 1), (5, 8)])
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_strides_and_addresses(dtype, order, pad, shift):
+    g = gen(pad * 10 + shift)
+    for kn, ci, t in [(1000, 64, 80), (515, 72, 7), (300, 40, 200)]:
+        F, X, b = layer(g, kn, ci, t, dtype, order, pad=pad, shift=shift)
+        check(F, X, b, {"labels": labels_of(g, kn, t), "ignore": IGNORE}, gradient_of(g, t))
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_several_pieces(dtype, order):
+    """More classes than a piece of the gradients holds, the last piece ragged (order 1)
+    or a few classes long; entries of a teacher on both sides of each border."""
+    g = gen(5)
+    t = 2200 if dtype == torch.float32 else 4400
+    kn = 17000 if order == 0 else 16411
+    F, X, b = layer(g, kn, 40, t, dtype, order)
+    check(F, X, b, {"labels": labels_of(g, kn, t), "ignore": IGNORE}, gradient_of(g, t))
+    border = -(-kn // 2 // 256) * 256 if kn > 16384 else 8192
+    top, index = teacher_of(g, kn, t, 9, dtype)
+    index[3:9] = torch.tensor([0, kn - 1, 5631, 5632, 8191, 8192], device="cuda")[:, None]
+    assert border > 0
+    check(F, X, b, {"top": top, "index": index, "temperature": 4.0}, gradient_of(g, t))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_masked_classes(dtype):
+    """Classes with a bias of -infinity, whole tiles of them among these, or of the type's
+    lowest value: p = 0, no gradient; a masked label's loss is infinite."""
+    g = gen(11)
+    kn, ci, t = 1000, 64, 80
+    F, X, b = layer(g, kn, ci, t, dtype, 1)
+    for low in (-torch.inf, torch.finfo(dtype).min):
+        b2 = b.clone()
+        b2[:400] = low
+        b2[777] = low
+        y = torch.randint(400, 777, (t,), generator=g, device="cuda")
+        case = {"labels": y, "ignore": IGNORE}
+        loss, lse = forward(F, X, b2, case)
+        keep = [i for i in range(400, kn) if i != 777]
+        rest = {"labels": y - 400, "ignore": IGNORE}
+        want = truth.forward(F[keep], X, b2[keep], rest)
+        for got, w, bound in zip((loss, lse), want, truth.forward_bound(F[keep], X, b2[keep], rest)):
+            within(got, w, bound, "masked")
+        gr = gradient_of(g, t)
+        dX, dF, db = backward(F, X, b2, case, lse, gr)
+        for got, w, bound in zip((dX, dF[keep], db[keep]), truth.backward(F[keep], X, b2[keep], rest, gr),
+                                 truth.backward_bound(F[keep], X, b2[keep], rest, gr, dtype)):
+            within(got, w, bound, "masked")
+        assert not dF[:400].any() and not db[:400].any() and not db[777]
+    b2 = b.clone()
+    b2[3] = -torch.inf
+    loss, lse = forward(F, X, b2, {"labels": torch.full((t,), 3, device="cuda"), "ignore": IGNORE})
+    assert (loss == torch.inf).all() and lse.isfinite().all()
+    # nothing left at all
+    loss, lse = forward(F, X, torch.full_like(b, -torch.inf), {"labels": torch.full((t,), 3, device="cuda"), "ignore": IGNORE})
+    assert (lse == -torch.inf).all() and loss.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_columns_that_do_not_count(dtype):
+    """Ignored columns and columns with g = 0 hold infinities and NaN: loss 0 (where
+    ignored), and no trace in any gradient.  Labels beyond the classes give NaN."""
+    g = gen(12)
+    kn, ci, t = 700, 72, 90
+    F, X, b = layer(g, kn, ci, t, dtype, 0)
+    y = labels_of(g, kn, t, ignored=0.0)
+    y[::5] = IGNORE
+    gr = gradient_of(g, t)
+    gr[1::5] = 0.0
+    Xn = X.clone()
+    Xn[:, ::5] = torch.nan
+    Xn[3, 1::5] = torch.inf
+    case = {"labels": y, "ignore": IGNORE}
+    loss, lse = forward(F, Xn, b, case)
+    assert (loss[::5] == 0).all() and loss[2::5].isfinite().all()
+    clean = backward(F, X, b, case, forward(F, X, b, case)[1], gr)
+    dirty = backward(F, Xn, b, case, lse, gr)
+    for a, c in zip(dirty, clean):
+        assert torch.equal(a, c)
+    assert not dirty[0][:, ::5].any() and not dirty[0][:, 1::5].any()
+    for wrong in (kn, -1, 1 << 40):
+        y2 = y.clone()
+        y2[7] = wrong
+        loss, lse = forward(F, X, b, {"labels": y2, "ignore": IGNORE})
+        assert loss[7].isnan() and int(loss.isnan().sum()) == 1 and lse.isfinite().all()
+        dX, dF, db = backward(F, X, b, {"labels": y2, "ignore": IGNORE}, lse, gradient_of(g, t))
+        assert dX[:, 7].isnan().all() and dX[:, :7].isfinite().all() and dX[:, 8:].isfinite().all()
+        assert dF.isnan().all() and db.isnan().all()
+    # every column ignored: zeros, also where X is NaN
+    none = {"labels": torch.full((t,), IGNORE, device="cuda"), "ignore": IGNORE}
+    loss, lse = forward(F, Xn, b, none)
+    assert not loss.any()
+    for v in backward(F, Xn, b, none, lse, gr):
+        assert not v.any()
+
+
+def test_teacher_entries():
+    """An index beyond the classes, a NaN or two infinite logits give NaN in their
+    column alone; an entry that does not count may hold anything."""
+    g = gen(13)
+    kn, ci, t, k = 500, 64, 12, 6
+    F, X, b = layer(g, kn, ci, t, torch.float32, 1)
+    top, index = teacher_of(g, kn, t, k, torch.float32)
+    index[0] = torch.arange(t, device="cuda")
+    top, index = top.contiguous().t().contiguous().t(), index.t().contiguous().t()
+    base = forward(F, X, b, {"top": top, "index": index, "temperature": 1.0})[0]
+    top2, index2 = top.clone(), index.clone()
+    index2[4, 3] = kn
+    top2[4, 5] = torch.nan
+    top2[4:6, 7] = torch.inf
+    index2[4:6, 7] = torch.tensor([1, 2], device="cuda")
+    index2[3, 9], top2[3, 9] = -5, torch.nan
+    index2[5, 10], top2[5, 10] = 1 << 30, -torch.inf
+    index2[4, 5] = 3
+    loss, lse = forward(F, X, b, {"top": top2, "index": index2, "temperature": 1.0})
+    assert loss[[3, 5, 7]].isnan().all() and int(loss.isnan().sum()) == 3 and lse.isfinite().all()
+    same = [0, 1, 4, 6, 8, 11]
+    assert torch.equal(loss[same], base[same])
+    dX, dF, db = lt().linear_distill_backward(F, X, top2, index2, lse, torch.ones(t, device="cuda"), bias=b)
+    fine = [i for i in range(t) if i not in (3, 5, 7)]
+    assert dX[:, fine].isfinite().all() and dX[:, 3].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_label_is_a_teacher_of_one(dtype):
+    """k = 1 at T = 1 is cross entropy: the same bits."""
+    g = gen(14)
+    F, X, b = layer(g, 1003, 72, 50, dtype, 1)
+    y = labels_of(g, 1003, 50, ignored=0.0)
+    gr = gradient_of(g, 50)
+    a = lt().linear_cross_entropy(F, X, y, bias=b)
+    top = torch.randn(1, 50, generator=g, device="cuda")
+    c = lt().linear_distill(F, X, top, y[None], bias=b)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+    for u, v in zip(lt().linear_cross_entropy_backward(F, X, y, a[1], gr, bias=b),
+                    lt().linear_distill_backward(F, X, top, y[None], c[1], gr, bias=b)):
+        assert torch.equal(u, v)
+
+
+def test_gradients_are_differences():
+    """Central differences of the library's own losses (fp32) along random directions:
+    h^2 of the third derivative and the losses' error over h."""
+    g = gen(15)
+    kn, ci, t, k, h = 300, 40, 24, 7, 2.0 ** -6
+    F, X, b = layer(g, kn, ci, t, torch.float32, 1)
+    top, index = teacher_of(g, kn, t, k, torch.float32)
+    for case in ({"labels": labels_of(g, kn, t), "ignore": IGNORE}, {"top": top, "index": index, "temperature": 2.0}):
+        gr = gradient_of(g, t)
+        lse = forward(F, X, b, case)[1]
+        grads = backward(F, X, b, case, lse, gr)
+        for i, got in enumerate(grads):
+            args = [X, F, b]
+            d = torch.randn(args[i].shape, generator=g, device="cuda")
+            d = d / d.norm()
+            values, exact = [], []
+            for sign in (1, -1):
+                moved = list(args)
+                moved[i] = (args[i] + sign * h * d)
+                if i == 0:
+                    moved[0] = moved[0].t().contiguous().t()
+                values.append((forward(moved[1], moved[0], moved[2], case)[0].double() * gr.double()).sum())
+                exact.append((truth.forward(moved[1], moved[0], moved[2], case)[0] * gr.double()).sum())
+            bound = (gr.double().abs() * truth.forward_bound(F, X, b, case)[0]).sum() * 2 / h
+            # the truth's own difference carries the same h^2 error
+            assert abs((values[0] - values[1]) / (2 * h) - (exact[0] - exact[1]) / (2 * h)) <= 1.1 * bound
+            slope = float((got.double() * d.double()).sum())
+            assert abs(slope - float((exact[0] - exact[1]) / (2 * h))) <= 1e-2 * abs(slope) + 1e-4
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_outputs_that_are_left_out(dtype):
+    g = gen(16)
+    for kn, ci, t, order in [(1000, 64, 80, 1), (515, 33, 7, 0)]:
+        F, X, b = layer(g, kn, ci, t, dtype, order)
+        case, gr = {"labels": labels_of(g, kn, t), "ignore": IGNORE}, gradient_of(g, t)
+        lse = forward(F, X, b, case)[1]
+        every = backward(F, X, b, case, lse, gr)
+        for needs in [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (0, 1, 1), (1, 0, 1), (0, 0, 0)]:
+            got = backward(F, X, b, case, lse, gr, needs=needs)
+            for n, a, v in zip(needs, got, every):
+                assert (a is None) == (not n)
+                if n:
+                    assert torch.equal(a, v)
+
+
+def test_one_gradient_for_all_tokens():
+    g = gen(17)
+    F, X, b = layer(g, 400, 32, 60, torch.bfloat16, 1)
+    y = labels_of(g, 400, 60)
+    lse = lt().linear_cross_entropy(F, X, y, bias=b)[1]
+    one = torch.tensor(0.125, device="cuda")
+    want = lt().linear_cross_entropy_backward(F, X, y, lse, one.expand(60).contiguous(), bias=b)
+    for given in (one, one.expand(60)):
+        for a, v in zip(lt().linear_cross_entropy_backward(F, X, y, lse, given, bias=b), want):
+            assert torch.equal(a, v)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_small_and_large_gradients(dtype):
+    """Gradients far from 1, which fp16 holds relative to a power of two."""
+    g = gen(18)
+    F, X, b = layer(g, 900, 48, 64, dtype, 0)
+    case = {"labels": labels_of(g, 900, 64), "ignore": IGNORE}
+    lse = forward(F, X, b, case)[1]
+    base = torch.rand(64, generator=g, device="cuda") + 0.5
+    for size in (2.0 ** -20, 2.0 ** 6):
+        gr = base * size
+        got = backward(F, X, b, case, lse, gr)
+        for a, want, bound in zip(got, truth.backward(F, X, b, case, gr), truth.backward_bound(F, X, b, case, gr, dtype)):
+            within(a, want, bound, f"g about {size}")
+
+
+def test_empty_extents():
+    g = gen(19)
+    y = torch.zeros(0, dtype=torch.int64, device="cuda")
+    F, X, b = layer(g, 40, 16, 0, torch.bfloat16, 1)
+    loss, lse = lt().linear_cross_entropy(F, X, y, bias=b)
+    assert loss.shape == lse.shape == (0,)
+    dX, dF, db = lt().linear_cross_entropy_backward(F, X, y, lse, lse, bias=b)
+    assert dX.shape == (16, 0) and not dF.any() and not db.any()
+    # no features: the bias alone
+    y = torch.tensor([1, 2, IGNORE], device="cuda")
+    for dtype in DTYPES:
+        F, X, b = torch.empty(40, 0, dtype=dtype, device="cuda"), torch.empty(3, 0, dtype=dtype, device="cuda").t(), torch.randn(40, generator=g, device="cuda").to(dtype)
+        case, gr = {"labels": y, "ignore": IGNORE}, torch.ones(3, device="cuda")
+        check(F, X, b, case, gr)
+    # no classes: no label is valid
+    F, X = torch.empty(0, 16, device="cuda"), stored(g, 16, 3, torch.float32)
+    loss, lse = lt().linear_cross_entropy(F, X, y)
+    assert loss[:2].isnan().all() and loss[2] == 0 and (lse == -torch.inf).all()
+    dX, dF, db = lt().linear_cross_entropy_backward(F, X, y, lse, gr)
+    assert not dX.any() and dF.shape == (0, 16) and db.shape == (0,)
+
+
+def test_streams_graphs_and_repeats():
+    """The same bits on another stream, from two captured graphs that are replayed in
+    turn with eager calls between, and from call to call."""
+    g = gen(20)
+    cases = []
+    for kn, ci, t, dtype, order in [(1500, 64, 130, torch.bfloat16, 1), (700, 40, 9, torch.float16, 0)]:
+        F, X, b = layer(g, kn, ci, t, dtype, order)
+        top, index = teacher_of(g, kn, t, 5, dtype)
+        cases.append((F, X, b, {"top": top, "index": index, "temperature": 2.0}, gradient_of(g, t)))
+
+    def step(c):
+        F, X, b, case, gr = c
+        loss, lse = forward(F, X, b, case)
+        return (loss, lse) + tuple(backward(F, X, b, case, lse, gr))
+
+    want = [step(c) for c in cases]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = [step(c) for c in cases]
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, held = [], []
+    for c in cases:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(step(c))
+        graphs.append(graph)
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        again = [step(c) for c in cases]
+        torch.cuda.synchronize()
+        for w, h, a, o in zip(want, held, again, other):
+            for x, y, z, v in zip(w, h, a, o):
+                assert torch.equal(x, y) and torch.equal(x, z) and torch.equal(x, v)
+        for h in held:
+            for v in h:
+                v.zero_()
+
+
+def test_refusals():
+    g = gen(21)
+    F, X, b = layer(g, 50, 16, 6, torch.bfloat16, 1)
+    y = labels_of(g, 50, 6)
+    top, index = teacher_of(g, 50, 6, 4, torch.bfloat16)
+    m = lt()
+    lse = torch.zeros(6, device="cuda")
+    bad = [
+        (ValueError, lambda: m.linear_cross_entropy(F, X, y[:5])),
+        (TypeError, lambda: m.linear_cross_entropy(F, X, y.float())),
+        (TypeError, lambda: m.linear_cross_entropy(F, X, y.short())),
+        (ValueError, lambda: m.linear_cross_entropy(F, X, y.cpu())),
+        (ValueError, lambda: m.linear_cross_entropy(F, X, torch.stack([y, y], 1)[:, 0])),
+        (ValueError, lambda: m.linear_cross_entropy(F, X, y, bias=b[:49])),
+        (TypeError, lambda: m.linear_cross_entropy(F, X, y, bias=b.float())),
+        (ValueError, lambda: m.linear_cross_entropy(F, X[:15], y)),
+        (TypeError, lambda: m.linear_cross_entropy(F.float(), X, y)),
+        (TypeError, lambda: m.linear_cross_entropy(F.double(), X.double(), y)),
+        (ValueError, lambda: m.linear_cross_entropy_backward(F, X, y, lse[:5], lse)),
+        (ValueError, lambda: m.linear_cross_entropy_backward(F, X, y, lse, lse[:5])),
+        (TypeError, lambda: m.linear_cross_entropy_backward(F, X, y, lse, lse.double())),
+        (TypeError, lambda: m.linear_cross_entropy_backward(F, X, y, lse.half(), lse)),
+        (ValueError, lambda: m.linear_cross_entropy_backward(F, X, y, lse, torch.tensor(1.0))),
+        (ValueError, lambda: m.linear_distill(F, X, top, index[:3])),
+        (ValueError, lambda: m.linear_distill(F, X, top.t().contiguous(), index)),
+        (ValueError, lambda: m.linear_distill(F, X, top.contiguous(), index)),
+        (TypeError, lambda: m.linear_distill(F, X, top.double(), index)),
+        (TypeError, lambda: m.linear_distill(F, X, top, index.float())),
+        (ValueError, lambda: m.linear_distill(F, X, top, index, temperature=0.0)),
+        (ValueError, lambda: m.linear_distill(F, X, top, index, temperature=float("nan"))),
+        (ValueError, lambda: m.linear_distill(F, X, top, index, temperature=float("inf"))),
+        (ValueError, lambda: m.linear_distill(F, X, top[:0], index[:0])),
+        (ValueError, lambda: m.linear_distill(F, X, torch.zeros(6, 1025, device="cuda").t(), torch.zeros(6, 1025, device="cuda", dtype=torch.int64).t())),
+    ]
+    for error, call in bad:
+        with pytest.raises(error):
+            call()
