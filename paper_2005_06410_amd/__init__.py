@@ -54,6 +54,8 @@ __all__ = [
     "linear_cross_entropy_backward",
     "linear_distill",
     "linear_distill_backward",
+    "group_norm",
+    "group_norm_backward",
     "LtltError",
     "F64",
     "F32",
@@ -72,6 +74,8 @@ _LABELS = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64]
 _TEACHER = [ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64] * 2 + [ctypes.c_double]
 _GRADIENTS = ([ctypes.c_void_p] * 2 + [ctypes.c_int] + [ctypes.c_void_p, ctypes.c_int64] * 2 + [ctypes.c_void_p] * 2
               + [ctypes.c_int64, ctypes.c_void_p])
+# include/group_norm.h: a tensor with its distances between positions and images
+_MAP = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64]
 
 _SYMBOLS = {
     "ltlt_factor": ([ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p,
@@ -130,6 +134,15 @@ _SYMBOLS = {
     "convgemm_linear_distill": (_LAYER + _TEACHER + [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
     "convgemm_linear_cross_entropy_backward": (_LAYER + _LABELS + _GRADIENTS, ctypes.c_int),
     "convgemm_linear_distill_backward": (_LAYER + _TEACHER + _GRADIENTS, ctypes.c_int),
+    # include/group_norm.h
+    "convgemm_group_norm_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 4, ctypes.c_int64),
+    "convgemm_group_norm_backward_workspace": ([ctypes.c_int] + [ctypes.c_int64] * 4, ctypes.c_int64),
+    "convgemm_group_norm": ([ctypes.c_int] + [ctypes.c_int64] * 4 + _MAP + [ctypes.c_void_p] * 2
+                            + [ctypes.c_double, ctypes.c_int] + _MAP + [ctypes.c_void_p] * 3
+                            + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
+    "convgemm_group_norm_backward": ([ctypes.c_int] + [ctypes.c_int64] * 4 + _MAP * 2 + [ctypes.c_void_p] * 2
+                                     + [ctypes.c_int] + [ctypes.c_void_p] * 2 + _MAP + [ctypes.c_void_p] * 3
+                                     + [ctypes.c_int64, ctypes.c_void_p], ctypes.c_int),
 }
 
 
@@ -871,6 +884,145 @@ def linear_distill_backward(F, X, top, index, lse, dloss, bias=None, temperature
     layer = _loss_layer(F, X, bias)
     k, target = _teacher_args(top, index, layer[2], temperature, layer[4])
     return _loss_backward("convgemm_linear_distill_backward", layer, k, target, X, lse, dloss, needs)
+
+
+def _map_strides(v, shape, name: str, dtype, dev: int):
+    """(distance between positions, between images) of a (c, ..., b) tensor stored with
+    its first index fastest and its positions evenly apart."""
+    if v.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    if v.dtype != dtype:
+        raise TypeError(f"{name} must have I's dtype")
+    if v.get_device() != dev:
+        raise ValueError("all tensor arguments must be on the same GPU")
+    c, b, strides = shape[0], shape[-1], v.stride()
+    if 0 in shape:
+        positions = 1
+        for size in shape[1:-1]:
+            positions *= size
+        return max(c, 1), max(positions * max(c, 1), c)
+    ld, step, s = None, None, 1
+    for size, stride in zip(shape[1:-1], strides[1:-1]):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = step = stride
+        if stride != step:
+            raise ValueError(f"{name}'s positions must be evenly apart, the leftmost index fastest")
+        step = stride * size
+        s *= size
+    ld = max(c, 1) if ld is None else ld
+    ldb = strides[-1] if b > 1 else (s - 1) * ld + max(c, 1)
+    if (c > 1 and strides[0] != 1) or ld < c or (b > 1 and ldb < (s - 1) * ld + c):
+        raise ValueError(f"{name} must be stored leftmost index fastest, without overlap")
+    return ld, ldb
+
+
+def _norm_args(I, groups: int, weight, bias, activation: str):
+    _require_gpu(I)
+    if I.dim() < 2:
+        raise ValueError("I must be (c, ..., b)")
+    dtype, dev = I.dtype, I.get_device()
+    code, c, b, s = _layer_dtype(dtype), I.shape[0], I.shape[-1], 1
+    for size in I.shape[1:-1]:
+        s *= size
+    groups = int(groups)
+    if groups < 1 or c % groups or groups > max(c, 1):
+        raise ValueError("groups must divide the channels")
+    act = _activation(activation)
+    for v, name in ((weight, "weight"), (bias, "bias")):
+        if v is None:
+            continue
+        if v.shape != (c,) or (c > 1 and v.stride(0) != 1):
+            raise ValueError(f"{name} must be a contiguous tensor of {c} values")
+        if v.dtype != dtype:
+            raise TypeError(f"{name} must have I's dtype")
+        if v.get_device() != dev:
+            raise ValueError("all tensor arguments must be on the same GPU")
+    return (code, c, s, b, groups), act, dtype, dev
+
+
+def _new_map(I):
+    """A tensor like I, stored with the leftmost index fastest."""
+    strides, step = [], 1
+    for size in I.shape:
+        strides.append(step)
+        step *= max(size, 1)
+    return I.new_empty_strided(tuple(I.shape), tuple(strides))
+
+
+def _map_span(v, ld: int, ldb: int, s: int):
+    return v.data_ptr(), v.data_ptr() + ((max(v.shape[-1], 1) - 1) * ldb + (max(s, 1) - 1) * ld + v.shape[0]) * v.element_size()
+
+
+def _over(a, b) -> bool:
+    return a[0] < b[1] and b[0] < a[1]
+
+
+def group_norm(I, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", out=None):
+    """O = act(weight (I - mean) rstd + bias), mean and variance over each of ``groups``
+    runs of channels and all positions of an image (``convgemm_group_norm``).
+
+    I: (c, ..., b), channels first and stored fastest, images last: what ``convgemm``
+    returns, (kn, ho, wo, b), or (c, t) for features of tokens; float32, bfloat16 or
+    float16, positions evenly apart.  ``weight`` and ``bias``: (c,), of I's dtype.
+    ``activation``: none, relu, gelu, gelu_tanh or silu.  Returns (O, mean, rstd): O like I
+    (``out`` if given; it may be I itself and overlap no other input), mean and rstd
+    (groups, b) float32, what ``group_norm_backward`` takes.  Nothing is recorded for
+    torch's automatic differentiation."""
+    sizes, act, dtype, dev = _norm_args(I, groups, weight, bias, activation)
+    eps = float(eps)
+    if not 0 <= eps < 1e38:
+        raise ValueError("eps must be at least 0 and finite")
+    ld, ldb = _map_strides(I, I.shape, "I", dtype, dev)
+    code, c, s, b, groups = sizes
+    if out is None:
+        out = _new_map(I)
+        ldo, ldbo = max(c, 1), max(c, 1) * max(s, 1)
+    else:
+        ldo, ldbo = _map_strides(out, I.shape, "out", dtype, dev)
+        if out.numel():
+            span = _map_span(out, ldo, ldbo, s)
+            itself = out.data_ptr() == I.data_ptr() and ldo == ld and (ldbo == ldb or b == 1)
+            if (not itself and _over(span, _map_span(I, ld, ldb, s))) or any(
+                    v is not None and _over(span, (v.data_ptr(), v.data_ptr() + c * v.element_size())) for v in (weight, bias)):
+                raise ValueError("out may not overlap an input other than I itself")
+    mean, rstd = (I.new_empty_strided((groups, b), (1, groups), dtype=_torch().float32) for _ in range(2))
+    need = _scratch_bytes("convgemm_group_norm_workspace", dev, *sizes)
+    ws = _scratch(need, I) if need else None
+    _launch("convgemm_group_norm", dev, *sizes, I.data_ptr(), ld, ldb, weight.data_ptr() if weight is not None else 0,
+            bias.data_ptr() if bias is not None else 0, eps, act, out.data_ptr(), ldo, ldbo, mean.data_ptr(), rstd.data_ptr(),
+            ws.data_ptr() if need else 0, need)
+    return out, mean, rstd
+
+
+def group_norm_backward(I, dO, groups: int, mean, rstd, weight=None, bias=None, activation: str = "none",
+                        needs=(True, True, True)):
+    """(dI, dweight, dbias) of ``group_norm`` from dO = dL/dO and the mean and rstd that it
+    returned (``convgemm_group_norm_backward``).  dI is stored like I with no gaps; without
+    a weight or bias the derivative is still that by a weight of ones or a bias of zeros.
+    ``needs`` leaves out what is not wanted (None is returned in its place)."""
+    sizes, act, dtype, dev = _norm_args(I, groups, weight, bias, activation)
+    ld, ldb = _map_strides(I, I.shape, "I", dtype, dev)
+    lddo, ldbdo = _map_strides(dO, I.shape, "dO", dtype, dev)
+    code, c, s, b, groups = sizes
+    for v, name in ((mean, "mean"), (rstd, "rstd")):
+        if v.dtype != _torch().float32:
+            raise TypeError(f"{name} must be float32")
+        if v.shape != (groups, b) or (groups > 1 and v.stride(0) != 1) or (b > 1 and v.stride(1) != groups):
+            raise ValueError(f"{name} must be ({groups}, {b}), the first index fastest, without gaps")
+        if v.get_device() != dev:
+            raise ValueError("all tensor arguments must be on the same GPU")
+    dI = _new_map(I) if needs[0] else None
+    dw = I.new_empty(c) if needs[1] else None
+    db = I.new_empty(c) if needs[2] else None
+    need = _scratch_bytes("convgemm_group_norm_backward_workspace", dev, *sizes)
+    ws = _scratch(need, I) if need else None
+    _launch("convgemm_group_norm_backward", dev, *sizes, I.data_ptr(), ld, ldb, dO.data_ptr(), lddo, ldbdo,
+            weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, act, mean.data_ptr(),
+            rstd.data_ptr(), dI.data_ptr() if dI is not None else 0, max(c, 1), max(c, 1) * max(s, 1),
+            dw.data_ptr() if dw is not None else 0, db.data_ptr() if db is not None else 0, ws.data_ptr() if need else 0, need)
+    return dI, dw, db
 
 
 def _dense(t) -> bool:
