@@ -886,77 +886,86 @@ def linear_distill_backward(F, X, top, index, lse, dloss, bias=None, temperature
     return _loss_backward("convgemm_linear_distill_backward", layer, k, target, X, lse, dloss, needs)
 
 
-def _map_strides(v, shape, name: str, dtype, dev: int):
-    """(distance between positions, between images) of a (c, ..., b) tensor stored with
-    its first index fastest and its positions evenly apart."""
-    if v.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}")
-    if v.dtype != dtype:
-        raise TypeError(f"{name} must have I's dtype")
-    if v.get_device() != dev:
-        raise ValueError("all tensor arguments must be on the same GPU")
-    c, b, strides = shape[0], shape[-1], v.stride()
-    if 0 in shape:
-        positions = 1
-        for size in shape[1:-1]:
-            positions *= size
-        return max(c, 1), max(positions * max(c, 1), c)
-    ld, step, s = None, None, 1
+@functools.lru_cache(maxsize=1024)
+def _evenly_apart(shape, strides):
+    """(positions, distance between them, between images) of a (c, ..., b) tensor with its
+    first index fastest and its positions evenly apart, or None."""
+    c, b, s = shape[0], shape[-1], 1
+    for size in shape[1:-1]:
+        s *= size
+    if c * s * b == 0:
+        return s, max(c, 1), max(s * max(c, 1), c)
+    ld = step = None
     for size, stride in zip(shape[1:-1], strides[1:-1]):
         if size == 1:
             continue
         if ld is None:
             ld = step = stride
         if stride != step:
-            raise ValueError(f"{name}'s positions must be evenly apart, the leftmost index fastest")
+            return None
         step = stride * size
-        s *= size
-    ld = max(c, 1) if ld is None else ld
-    ldb = strides[-1] if b > 1 else (s - 1) * ld + max(c, 1)
+    ld = c if ld is None else ld
+    ldb = strides[-1] if b > 1 else (s - 1) * ld + c
     if (c > 1 and strides[0] != 1) or ld < c or (b > 1 and ldb < (s - 1) * ld + c):
-        raise ValueError(f"{name} must be stored leftmost index fastest, without overlap")
-    return ld, ldb
+        return None
+    return s, ld, ldb
+
+
+def _map_strides(v, shape, name: str, dtype, dev: int):
+    """(positions, distance between them, between images) of a map like I."""
+    if v.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    if v.dtype != dtype:
+        raise TypeError(f"{name} must have I's dtype")
+    if v.get_device() != dev:
+        raise ValueError("all tensor arguments must be on the same GPU")
+    got = _evenly_apart(v.shape, v.stride())
+    if got is None:
+        raise ValueError(f"{name} must be stored leftmost index fastest, its positions evenly apart and without overlap")
+    return got
 
 
 def _norm_args(I, groups: int, weight, bias, activation: str):
+    """(the C sizes, activation, dtype, GPU index, I's distances, and the addresses of
+    weight and bias)."""
     _require_gpu(I)
     if I.dim() < 2:
         raise ValueError("I must be (c, ..., b)")
-    dtype, dev = I.dtype, I.get_device()
-    code, c, b, s = _layer_dtype(dtype), I.shape[0], I.shape[-1], 1
-    for size in I.shape[1:-1]:
-        s *= size
+    dtype, dev, shape = I.dtype, I.get_device(), I.shape
+    code, c = _layer_dtype(dtype), shape[0]
+    s, ld, ldb = _map_strides(I, shape, "I", dtype, dev)
     groups = int(groups)
     if groups < 1 or c % groups or groups > max(c, 1):
         raise ValueError("groups must divide the channels")
     act = _activation(activation)
-    for v, name in ((weight, "weight"), (bias, "bias")):
+    ptrs = [0, 0]
+    for i, v in enumerate((weight, bias)):
         if v is None:
             continue
+        name = "bias" if i else "weight"
         if v.shape != (c,) or (c > 1 and v.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous tensor of {c} values")
         if v.dtype != dtype:
             raise TypeError(f"{name} must have I's dtype")
         if v.get_device() != dev:
             raise ValueError("all tensor arguments must be on the same GPU")
-    return (code, c, s, b, groups), act, dtype, dev
+        ptrs[i] = v.data_ptr()
+    return (code, c, s, shape[-1], groups), act, dtype, dev, (ld, ldb), ptrs
 
 
-def _new_map(I):
-    """A tensor like I, stored with the leftmost index fastest."""
+@functools.lru_cache(maxsize=1024)
+def _leftmost_strides(shape):
     strides, step = [], 1
-    for size in I.shape:
+    for size in shape:
         strides.append(step)
         step *= max(size, 1)
-    return I.new_empty_strided(tuple(I.shape), tuple(strides))
+    return tuple(strides)
 
 
-def _map_span(v, ld: int, ldb: int, s: int):
-    return v.data_ptr(), v.data_ptr() + ((max(v.shape[-1], 1) - 1) * ldb + (max(s, 1) - 1) * ld + v.shape[0]) * v.element_size()
-
-
-def _over(a, b) -> bool:
-    return a[0] < b[1] and b[0] < a[1]
+def _span(v, b: int, s: int, c: int, ld: int, ldb: int):
+    """The addresses between a map's first value and its last."""
+    at = v.data_ptr()
+    return at, at + ((b - 1) * ldb + (s - 1) * ld + c) * v.element_size()
 
 
 def group_norm(I, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", out=None):
@@ -970,29 +979,28 @@ def group_norm(I, groups: int, weight=None, bias=None, eps: float = 1e-5, activa
     (``out`` if given; it may be I itself and overlap no other input), mean and rstd
     (groups, b) float32, what ``group_norm_backward`` takes.  Nothing is recorded for
     torch's automatic differentiation."""
-    sizes, act, dtype, dev = _norm_args(I, groups, weight, bias, activation)
+    sizes, act, dtype, dev, dist, (wp, bp) = _norm_args(I, groups, weight, bias, activation)
     eps = float(eps)
     if not 0 <= eps < 1e38:
         raise ValueError("eps must be at least 0 and finite")
-    ld, ldb = _map_strides(I, I.shape, "I", dtype, dev)
-    code, c, s, b, groups = sizes
+    _, c, s, b, groups = sizes
     if out is None:
-        out = _new_map(I)
-        ldo, ldbo = max(c, 1), max(c, 1) * max(s, 1)
+        out = I.new_empty_strided(I.shape, _leftmost_strides(I.shape))
+        disto = (max(c, 1), max(c, 1) * max(s, 1))
     else:
-        ldo, ldbo = _map_strides(out, I.shape, "out", dtype, dev)
-        if out.numel():
-            span = _map_span(out, ldo, ldbo, s)
-            itself = out.data_ptr() == I.data_ptr() and ldo == ld and (ldbo == ldb or b == 1)
-            if (not itself and _over(span, _map_span(I, ld, ldb, s))) or any(
-                    v is not None and _over(span, (v.data_ptr(), v.data_ptr() + c * v.element_size())) for v in (weight, bias)):
+        disto = _map_strides(out, I.shape, "out", dtype, dev)[1:]
+        if c * s * b:
+            span, size = _span(out, b, s, c, *disto), I.element_size()
+            itself = out.data_ptr() == I.data_ptr() and disto[0] == dist[0] and (disto[1] == dist[1] or b == 1)
+            inputs = [(p, p + c * size) for p in (wp, bp) if p] + ([] if itself else [_span(I, b, s, c, *dist)])
+            if any(lo < span[1] and span[0] < hi for lo, hi in inputs):
                 raise ValueError("out may not overlap an input other than I itself")
-    mean, rstd = (I.new_empty_strided((groups, b), (1, groups), dtype=_torch().float32) for _ in range(2))
+    f32 = _torch().float32
+    mean, rstd = I.new_empty_strided((groups, b), (1, groups), dtype=f32), I.new_empty_strided((groups, b), (1, groups), dtype=f32)
     need = _scratch_bytes("convgemm_group_norm_workspace", dev, *sizes)
     ws = _scratch(need, I) if need else None
-    _launch("convgemm_group_norm", dev, *sizes, I.data_ptr(), ld, ldb, weight.data_ptr() if weight is not None else 0,
-            bias.data_ptr() if bias is not None else 0, eps, act, out.data_ptr(), ldo, ldbo, mean.data_ptr(), rstd.data_ptr(),
-            ws.data_ptr() if need else 0, need)
+    _launch("convgemm_group_norm", dev, *sizes, I.data_ptr(), *dist, wp, bp, eps, act, out.data_ptr(), *disto, mean.data_ptr(),
+            rstd.data_ptr(), ws.data_ptr() if need else 0, need)
     return out, mean, rstd
 
 
@@ -1002,10 +1010,9 @@ def group_norm_backward(I, dO, groups: int, mean, rstd, weight=None, bias=None, 
     returned (``convgemm_group_norm_backward``).  dI is stored like I with no gaps; without
     a weight or bias the derivative is still that by a weight of ones or a bias of zeros.
     ``needs`` leaves out what is not wanted (None is returned in its place)."""
-    sizes, act, dtype, dev = _norm_args(I, groups, weight, bias, activation)
-    ld, ldb = _map_strides(I, I.shape, "I", dtype, dev)
-    lddo, ldbdo = _map_strides(dO, I.shape, "dO", dtype, dev)
-    code, c, s, b, groups = sizes
+    sizes, act, dtype, dev, dist, (wp, bp) = _norm_args(I, groups, weight, bias, activation)
+    distd = _map_strides(dO, I.shape, "dO", dtype, dev)[1:]
+    _, c, s, b, groups = sizes
     for v, name in ((mean, "mean"), (rstd, "rstd")):
         if v.dtype != _torch().float32:
             raise TypeError(f"{name} must be float32")
@@ -1013,15 +1020,21 @@ def group_norm_backward(I, dO, groups: int, mean, rstd, weight=None, bias=None, 
             raise ValueError(f"{name} must be ({groups}, {b}), the first index fastest, without gaps")
         if v.get_device() != dev:
             raise ValueError("all tensor arguments must be on the same GPU")
-    dI = _new_map(I) if needs[0] else None
-    dw = I.new_empty(c) if needs[1] else None
-    db = I.new_empty(c) if needs[2] else None
+    dI = dw = db = None
+    ip = wdp = bdp = 0
+    if needs[0]:
+        dI = I.new_empty_strided(I.shape, _leftmost_strides(I.shape))
+        ip = dI.data_ptr()
+    if needs[1]:
+        dw = I.new_empty(c)
+        wdp = dw.data_ptr()
+    if needs[2]:
+        db = I.new_empty(c)
+        bdp = db.data_ptr()
     need = _scratch_bytes("convgemm_group_norm_backward_workspace", dev, *sizes)
     ws = _scratch(need, I) if need else None
-    _launch("convgemm_group_norm_backward", dev, *sizes, I.data_ptr(), ld, ldb, dO.data_ptr(), lddo, ldbdo,
-            weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, act, mean.data_ptr(),
-            rstd.data_ptr(), dI.data_ptr() if dI is not None else 0, max(c, 1), max(c, 1) * max(s, 1),
-            dw.data_ptr() if dw is not None else 0, db.data_ptr() if db is not None else 0, ws.data_ptr() if need else 0, need)
+    _launch("convgemm_group_norm_backward", dev, *sizes, I.data_ptr(), *dist, dO.data_ptr(), *distd, wp, bp, act, mean.data_ptr(),
+            rstd.data_ptr(), ip, max(c, 1), max(c, 1) * max(s, 1), wdp, bdp, ws.data_ptr() if need else 0, need)
     return dI, dw, db
 
 
