@@ -190,8 +190,23 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
+// f(chunk, channel of the group) for a group's chunks and channels, dealt out to 256
+// threads.
+template <class F> __device__ inline void each_entry(const Norm& a, F f) {
+  if (a.per >= 256) {
+    for (int k = 0; k < a.chunks; ++k)
+      for (int i = threadIdx.x; i < a.per; i += 256) f(k, i);
+  } else {
+    const int lines = 256 / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
+    if (line < lines) {
+#pragma unroll 4
+      for (int k = line; k < a.chunks; k += lines) f(k, i);
+    }
+  }
+}
+
 // The groups' mean and rstd from their chunks and channels.
-__global__ __launch_bounds__(256) void norm_join_kernel(Norm a) {
+__global__ __launch_bounds__(256) void norm_groups_kernel(Norm a) {
   __shared__ float sh[4];
   for (int64_t id = blockIdx.x; id < a.b * a.groups; id += gridDim.x) {
     const int64_t n = id / a.groups;
@@ -256,7 +271,7 @@ template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, c
   norm_stats_kernel<T, MODE><<<grid, kSplitThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  norm_join_kernel<<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
+  norm_groups_kernel<<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (streamed<T>(a))
     norm_apply_kernel<T, MODE, true><<<grid, kSplitThreads, 0, s>>>(a);

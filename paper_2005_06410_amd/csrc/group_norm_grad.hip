@@ -280,22 +280,54 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
-// The groups' avg d and avg(d xhat).
+// The sums of a group's channels over its chunks (to a.images), and from them the
+// group's avg d and avg(d xhat).  Narrow groups have 256 / per threads for a channel.
 template <class T> __global__ __launch_bounds__(256) void norm_averages_kernel(Norm a) {
-  __shared__ float sh[4];
+  __shared__ float sh[4], line_s[256], line_x[256];
+  const int lines = a.per < 256 ? 256 / a.per : 1;
+  const int line = a.per < 256 ? threadIdx.x / a.per : 0, i0 = threadIdx.x - line * a.per;
   for (int64_t id = blockIdx.x; id < a.b * a.groups; id += gridDim.x) {
     const int64_t n = id / a.groups, g = id - n * a.groups;
     const float* from = a.sums + n * a.chunks * a.c + g * a.per;
-    float s = 0.0f, sx = 0.0f;
-    each_entry(a, [&](int k, int i) {
-      const float w = a.weight ? (float)static_cast<const T*>(a.weight)[g * a.per + i] : 1.0f;
-      s += w * from[(int64_t)k * a.c + i];
-      sx += w * from[(a.parts + k) * a.c + i];
-    });
-    const float all = (float)a.per * (float)a.s;
-    s = block_sum(s, sh) / all;
-    sx = block_sum(sx, sh) / all;
-    if (threadIdx.x == 0) a.part[id] = float2{s, sx};
+    float all_s = 0.0f, all_x = 0.0f;
+    for (int i = i0; i < a.per; i += 256) {
+      float s = 0.0f, sx = 0.0f;
+      if (line < lines) {
+#pragma unroll 4
+        for (int k = line; k < a.chunks; k += lines) {
+          s += from[(int64_t)k * a.c + i];
+          sx += from[(a.parts + k) * a.c + i];
+        }
+      }
+      if (lines > 1) {
+        line_s[threadIdx.x] = s;
+        line_x[threadIdx.x] = sx;
+        __syncthreads();
+        if (line == 0)
+          for (int k = 1; k < lines; ++k) {
+            s += line_s[k * a.per + i];
+            sx += line_x[k * a.per + i];
+          }
+      }
+      if (line == 0) {
+        if (a.images) {
+          a.images[n * a.c + g * a.per + i] = s;
+          a.images[(a.b + n) * a.c + g * a.per + i] = sx;
+        }
+        const float w = a.weight ? (float)static_cast<const T*>(a.weight)[g * a.per + i] : 1.0f;
+        all_s += w * s;
+        all_x += w * sx;
+      }
+    }
+    if (!a.o.p) {
+      __syncthreads();
+      continue;
+    }
+    const float count = (float)a.per * (float)a.s;
+    all_s = block_sum(all_s, sh) / count;
+    all_x = block_sum(all_x, sh) / count;
+    if (threadIdx.x == 0) a.part[id] = float2{all_s, all_x};
+    __syncthreads();
   }
 }
 
@@ -349,9 +381,13 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
   const dim3 grid = grid_of(a.b * p.chunks * p.units);
   norm_slopes_kernel<T, MODE><<<grid, kSplitThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.o.p) return e;
+  if (e != hipSuccess) return e;
+  a.images = want ? reinterpret_cast<float*>(ws + p.images) : nullptr;
   norm_averages_kernel<T><<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  // dweight and dbias go on from the images' sums
+  a.sums = a.images;
+  a.parts = a.b;
+  if ((e = hipGetLastError()) != hipSuccess || !a.o.p) return e;
   if (streamed<T>(a))
     norm_dx_kernel<T, MODE, true><<<grid, kSplitThreads, 0, s>>>(a);
   else

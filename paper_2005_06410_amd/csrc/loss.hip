@@ -16,44 +16,102 @@ namespace {
 // exp(-inf) = 0 are then what the formula says, and nothing is inf - inf.
 __device__ inline float base_of(float top) { return fabsf(top) < INFINITY ? top : 0.0f; }
 
+// The loss of one column a workgroup from partial products.
+template <class T> __global__ __launch_bounds__(256) void shared_loss_kernel(LossProduct p, int splits) {
+  __shared__ float sh[4];
+  const int n = blockIdx.x;
+  auto over = [&](float v, auto f) {
+    for (int d = 32; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return f(f(sh[0], sh[1]), f(sh[2], sh[3]));
+  };
+  auto most = [](float a, float b) { return fmaxf(a, b); };
+  auto plus = [](float a, float b) { return a + b; };
+  float top = -INFINITY, sum = 0.0f;
+  for (int m = threadIdx.x * 4; m < p.M; m += 1024) {
+    float z[4];
+    shared_logits<T, 4>(p, splits, n, m, p.M - m, z);
+    const float t = fmaxf(top, fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
+    sum = top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(t));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += expf(z[i] - base_of(t));
+    top = t;
+  }
+  const float all = over(top, most);
+  sum = over(top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(all)), plus);
+  const float l = base_of(all) + logf(sum);
+  if (threadIdx.x == 0) p.lse_out[n] = l;
+  auto logit = [&](int64_t c) {
+    float z[4];
+    shared_logits<T, 4>(p, splits, n, (int)c, 1, z);
+    return z[0];
+  };
+  if (p.y.label) {
+    const int64_t label = label_of(p.y, n);
+    if (threadIdx.x == 0) p.loss[n] = label == p.y.ignore ? 0.0f : label >= 0 && label < p.kn ? l - logit(label) : NAN;
+    return;
+  }
+  const int count = p.y.count[n];
+  float v = 0.0f;
+  for (int e = threadIdx.x; e < count; e += 256) {
+    const int64_t i = (int64_t)n * p.y.k + e;
+    const float w = p.y.weight[i];
+    v += w == 0.0f ? 0.0f : w * (logf(w) - (logit(p.y.index[i]) - l));
+  }
+  v = over(v, plus);
+  if (threadIdx.x == 0) p.loss[n] = count < 0 ? NAN : count == 0 ? 0.0f : p.temperature2 * v;
+}
+
 // Ends a wave's tile with its columns' statistics.
 struct StatsEnd {
   using P = LossProduct;
+  template <class T> static hipError_t from_shares(const P& p, int splits, hipStream_t s) {
+    shared_loss_kernel<T><<<dim3((unsigned)p.N), 256, 0, s>>>(p, splits);
+    return hipGetLastError();
+  }
   template <class T, int VA, int VB, bool STREAM, int WM, int WN>
-  static __device__ void tile(const P& p, int, int m0, int n0, int lane, char*, f4 (&acc)[WM][WN]) {
+  static __device__ void tile(const P& p, int, int m0, int n0, int lane, char* lds, f4 (&acc)[WM][WN]) {
     static_assert(VB == 1, "X's contraction is contiguous");
-    constexpr int ROWS = 16 * WM;
+    constexpr int ROWS = 16 * WM, S = ROWS + 4;
     if (m0 >= p.M) return;
     const int q = lane >> 4, l16 = lane & 15;
-    const bool edge = m0 + ROWS > p.M;
-    const T* b = static_cast<const T*>(p.bias);
-    float bias[WM][4];
-    if (b) {
+    Entries entries[WN];
+#pragma unroll
+    for (int j = 0; j < WN; ++j) entries[j].find(p.y, n0 + 16 * j + l16, n0 + 16 * j + l16 < p.N, p.row0 + m0, ROWS);
+#pragma unroll
+    for (int j = 0; j < WN; ++j) entries[j].template first<false>(p.y, n0 + 16 * j + l16, p.row0 + m0, q);
+    by_plain(p, [&](auto plain) {
+      if constexpr (!decltype(plain)::value) {
+        float bias[WM][4];
+        bias_of<T, VA>(p, m0, q, bias);
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+          for (int j = 0; j < WN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = acc[i][j][r] * p.scale + bias[i][r];
+      }
+    });
+    if (m0 + ROWS > p.M) {
 #pragma unroll
       for (int i = 0; i < WM; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) bias[i][r] = p.scale * (float)b[min(m0 + row_of<VA>(i, r, q), p.M - 1)];
-    } else {
+        for (int r = 0; r < 4; ++r)
+          if (m0 + row_of<VA>(i, r, q) >= p.M) {
 #pragma unroll
-      for (int i = 0; i < WM; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) bias[i][r] = 0.0f;
+            for (int j = 0; j < WN; ++j) acc[i][j][r] = -INFINITY;
+          }
     }
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
       const int n = n0 + 16 * j + l16;
-      int lo, hi;
-      entries_of(p.y, n, n < p.N, p.row0 + m0, ROWS, lo, hi);
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < WM; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float z = acc[i][j][r] * p.scale + bias[i][r];
-          if (edge && m0 + row_of<VA>(i, r, q) >= p.M) z = -INFINITY;
-          acc[i][j][r] = z;
-          top = fmaxf(top, z);
-        }
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float base = base_of(top);
@@ -65,20 +123,25 @@ struct StatsEnd {
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (q == 0 && n < p.N) p.sums[(int64_t)(m0 / ROWS) * p.N + n] = float2{top, sum};
-      for (int e = lo; e < hi; ++e) {
-        const int64_t rel = entry_row(p.y, n, e, p.row0 + m0);
-        if (rel < 0 || rel >= ROWS) continue;
-        float z = 0.0f;
-        bool mine = false;
+      if (__any(entries[j].lo < entries[j].hi)) {
+        // a target's logit lies in some lane's register; through LDS it is one read away
+        float* st = reinterpret_cast<float*>(lds) + l16 * S;
 #pragma unroll
-        for (int i = 0; i < WM; ++i)
+        for (int i = 0; i < WM; ++i) {
+          if constexpr (VA == 1) {
+            *reinterpret_cast<f4*>(st + 16 * i + 4 * q) = acc[i][j];
+          } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool is = row_of<VA>(i, r, q) == (int)rel;
-            z = is ? acc[i][j][r] : z;
-            mine |= is;
+            for (int r = 0; r < 4; ++r) st[row_of<VA>(i, r, q)] = acc[i][j][r];
           }
-        if (mine) p.at[p.y.label ? (int64_t)n : (int64_t)n * p.y.k + e] = z;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        entries[j].template each<false>(p.y, n, p.row0 + m0, ROWS, 4, [&](int e, int row, float) {
+          p.at[p.y.label ? (int64_t)n : (int64_t)n * p.y.k + e] = st[row];
+        });
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
       }
     }
   }
@@ -92,7 +155,7 @@ template <int C>
 __global__ __launch_bounds__(256) void join_loss_kernel(int parts, int N, int64_t kn, const float2* __restrict__ sums,
                                                         const float* __restrict__ at, Targets y, float temperature2,
                                                         float* __restrict__ loss, float* __restrict__ lse) {
-  constexpr int LANES = 256 / C;
+  constexpr int LANES = 256 / C, AHEAD = 8;
   __shared__ float sh[LANES][C];
   const int c = threadIdx.x % C, x = threadIdx.x / C, n = blockIdx.x * C + c;
   const bool there = n < N;
@@ -108,25 +171,27 @@ __global__ __launch_bounds__(256) void join_loss_kernel(int parts, int N, int64_
     __syncthreads();
     return v;
   };
-  const float2* s = sums + n;
-  float top = -INFINITY;
-  if (there) {
-#pragma unroll 8
-    for (int r = x; r < parts; r += LANES) top = fmaxf(top, s[(int64_t)r * N].x);
-  }
-  top = over(top, [](float a, float b) { return fmaxf(a, b); });
-  const float base = base_of(top);
-  float sum = 0.0f;
-  if (there) {
-#pragma unroll 8
-    for (int r = x; r < parts; r += LANES) {
-      const float2 v = s[(int64_t)r * N];
-      // a part of -inf alone has the sum 0 (or NaN), whatever it is taken relative to
-      sum += v.x == -INFINITY ? v.y : v.y * expf(base_of(v.x) - base);
+  const float2* s = sums + min(n, N - 1);
+  float top = -INFINITY, sum = 0.0f;               // of this lane: sum is relative to top
+  for (int r0 = x; r0 < parts; r0 += AHEAD * LANES) {
+    float2 v[AHEAD];
+    float t = top;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int r = r0 + k * LANES;
+      v[k] = s[(int64_t)min(r, parts - 1) * N];
+      if (r >= parts) v[k] = float2{-INFINITY, 0.0f};
+      t = fmaxf(t, v[k].x);
     }
+    // a part of -inf alone has the sum 0 (or NaN), whatever it is taken relative to
+    sum = top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(t));
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) sum += v[k].x == -INFINITY ? v[k].y : v[k].y * expf(base_of(v[k].x) - base_of(t));
+    top = t;
   }
-  sum = over(sum, [](float a, float b) { return a + b; });
-  const float l = base + logf(sum);
+  const float all = over(top, [](float a, float b) { return fmaxf(a, b); });
+  sum = over(top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(all)), [](float a, float b) { return a + b; });
+  const float l = base_of(all) + logf(sum);
   if (y.label) {
     if (!there || x > 0) return;
     const int64_t label = label_of(y, n);
@@ -217,7 +282,7 @@ __global__ __launch_bounds__(64) void list_kernel(int64_t kn, int k, int size, c
 
 struct Forward {
   LossPlan plan;
-  int64_t copies, sums, at, lists, bytes;   // byte offsets
+  int64_t sums, at, lists, shares, bytes;   // byte offsets; copies first
   int parts;
 };
 
@@ -227,9 +292,11 @@ Forward forward_layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order
   w.parts = (int)ceil_div(kn, w.plan.rows);
   if (w.plan.route.copy_a) w.sums += up256(copy_values(dtype, f_order == 1, kn, ci) * type_size(dtype));
   if (w.plan.route.copy_b) w.sums += up256(copy_values(dtype, true, t, ci) * type_size(dtype));
-  w.at = w.sums + up256((int64_t)w.parts * t * 8);
-  w.lists = w.at + up256(t * std::max(k, 1) * 4);
-  w.bytes = w.lists + (k ? list_bytes(kn, t, k) : 0);
+  const bool whole = w.plan.splits == 1;
+  w.at = w.sums + (whole ? up256((int64_t)w.parts * t * 8) : 0);
+  w.lists = w.at + (whole ? up256(t * std::max(k, 1) * 4) : 0);
+  w.shares = w.lists + (k ? list_bytes(kn, t, k) : 0);
+  w.bytes = w.shares + share_bytes(w.plan, kn, t);
   return w;
 }
 
@@ -251,6 +318,11 @@ int loss_forward(const LossCall& c, float* loss, float* lse, char* ws, hipStream
   p.scale = (float)(1.0 / c.temperature);
   p.sums = reinterpret_cast<float2*>(ws + w.sums);
   p.at = reinterpret_cast<float*>(ws + w.at);
+  p.shares = reinterpret_cast<float*>(ws + w.shares);
+  p.kn = c.kn;
+  p.temperature2 = (float)(c.temperature * c.temperature);
+  p.loss = loss;
+  p.lse_out = lse;
   hipError_t e = hipSuccess;
   if (c.k)
     e = launch_lists(c, ws + w.lists, p.y, s);
@@ -258,11 +330,16 @@ int loss_forward(const LossCall& c, float* loss, float* lse, char* ws, hipStream
     p.y = Targets{c.labels, c.itype == LOSS_I64, c.ignore, nullptr, nullptr, nullptr, nullptr, 0, 0};
   if (e == hipSuccess && c.kn > 0) e = launch_loss<StatsEnd>(c.dtype, c.f_order == 1, p, ws, s);
   if (e != hipSuccess) return LINEAR_ERR_HIP_BASE - (int)e;
-  const float t2 = (float)(c.temperature * c.temperature);
-  if (c.t >= 256)
-    join_loss_kernel<16><<<dim3((unsigned)((c.t + 15) / 16)), 256, 0, s>>>(w.parts, p.N, c.kn, p.sums, p.at, p.y, t2, loss, lse);
+  if (w.plan.splits > 1) return LINEAR_OK;
+  auto join = [&](auto kernel, int columns) {
+    kernel<<<dim3((unsigned)((c.t + columns - 1) / columns)), 256, 0, s>>>(w.parts, p.N, c.kn, p.sums, p.at, p.y, p.temperature2, loss, lse);
+  };
+  if (c.t >= 2048)
+    join(join_loss_kernel<16>, 16);
+  else if (c.t >= 64)
+    join(join_loss_kernel<4>, 4);
   else
-    join_loss_kernel<1><<<dim3((unsigned)c.t), 256, 0, s>>>(w.parts, p.N, c.kn, p.sums, p.at, p.y, t2, loss, lse);
+    join(join_loss_kernel<1>, 1);
   e = hipGetLastError();
   return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
 }

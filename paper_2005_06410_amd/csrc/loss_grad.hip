@@ -11,10 +11,56 @@
 namespace linear {
 namespace {
 
+// dZ from partial products, and the sums of its rows over kSpan = 8 columns: 32 vectors of
+// a workgroup, each of whose eight groups of 32 lanes has a column.  Bound by latency, so
+// that nothing follows in one thread (64 columns a workgroup: 22 us instead of 5 at 80
+// columns of 1000 classes).
+template <class T> __global__ __launch_bounds__(256) void shared_dz_kernel(LossProduct p, int splits) {
+  constexpr int V = kVec<T>;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, m = (blockIdx.x * 32 + x) * V, cnt = p.M - m;
+  static_assert(kSpan == 8, "a column for each group of lanes");
+  const int n = blockIdx.y * kSpan + y;
+  float d[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) d[i] = 0.0f;
+  if (cnt > 0 && n < p.N) {
+    const float w = p.w[n], lse = p.lse[n];
+    Entries entries;
+    entries.find(p.y, n, w != 0.0f, p.row0 + m / kBin * kBin, kBin);
+    entries.first<true>(p.y, n, p.row0 + m / kBin * kBin, 0);
+    shared_logits<T, V>(p, splits, n, m, cnt, d);
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = w == 0.0f || i >= cnt ? 0.0f : w * exp_of<T>(d[i] - lse);
+    entries.each<true>(p.y, n, p.row0 + m / kBin * kBin, kBin, 1, [&](int, int row, float q) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[i] -= m % kBin + i == row && i < cnt ? w * q : 0.0f;
+    });
+    store_vec(static_cast<T*>(p.dZ) + (int64_t)n * p.lddz + m, d);
+  }
+  if (!p.db) return;
+  __shared__ float sh[8][32 * V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sh[y][x * V + i] = d[i];
+  __syncthreads();
+  for (int r = threadIdx.x; r < 32 * V; r += 256) {
+    const int k = blockIdx.x * 32 * V + r;
+    if (k >= p.M) break;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sh[i][r];
+    p.db[(int64_t)blockIdx.y * p.M + k] = s;
+  }
+}
+
 // Ends a wave's tile with dZ, and with the sums of its rows for dbias.  A column whose
 // w is 0 is written as zeros, whatever Z is there.
 struct SlopeEnd {
   using P = LossProduct;
+  template <class T> static hipError_t from_shares(const P& p, int splits, hipStream_t s) {
+    const int width = 32 * kVec<T>;
+    shared_dz_kernel<T><<<dim3((unsigned)((p.M + width - 1) / width), (unsigned)((p.N + kSpan - 1) / kSpan)), 256, 0, s>>>(p, splits);
+    return hipGetLastError();
+  }
   template <class T, int VA, int VB, bool STREAM, int WM, int WN>
   static __device__ void tile(const P& p, int, int m0, int n0, int lane, char* lds, f4 (&acc)[WM][WN]) {
     static_assert(VB == 1, "X's contraction is contiguous");
@@ -22,36 +68,41 @@ struct SlopeEnd {
     if (m0 >= p.M || n0 >= p.N) return;
     float* st = reinterpret_cast<float*>(lds);
     const int q = lane >> 4, l16 = lane & 15;
-    const T* b = static_cast<const T*>(p.bias);
-    float bias[WM][4];
-    if (b) {
+    Entries entries[WN];
+    float w[WN], lse[WN];
 #pragma unroll
-      for (int i = 0; i < WM; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) bias[i][r] = p.scale * (float)b[min(m0 + row_of<VA>(i, r, q), p.M - 1)];
-    } else {
-#pragma unroll
-      for (int i = 0; i < WM; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) bias[i][r] = 0.0f;
+    for (int j = 0; j < WN; ++j) {
+      const int n = n0 + 16 * j + l16;
+      entries[j].find(p.y, n, n < p.N, p.row0 + m0, ROWS);
+      w[j] = n < p.N ? p.w[n] : 0.0f;
+      lse[j] = n < p.N ? p.lse[n] : 0.0f;
     }
+#pragma unroll
+    for (int j = 0; j < WN; ++j) entries[j].template first<true>(p.y, n0 + 16 * j + l16, p.row0 + m0, 0);
+    by_plain(p, [&](auto plain) {
+      if constexpr (!decltype(plain)::value) {
+        float bias[WM][4];
+        bias_of<T, VA>(p, m0, q, bias);
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+          for (int j = 0; j < WN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = acc[i][j][r] * p.scale + bias[i][r];
+      }
+    });
     float total[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) total[i] = 0.0f;
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
       const int n = n0 + 16 * j + l16;
-      int lo, hi;
-      entries_of(p.y, n, n < p.N, p.row0 + m0, ROWS, lo, hi);
-      const float w = n < p.N ? p.w[n] : 0.0f, lse = n < p.N ? p.lse[n] : 0.0f;
 #pragma unroll
       for (int i = 0; i < WM; ++i) {
         float d[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float z = acc[i][j][r] * p.scale + bias[i][r];
-          d[r] = w == 0.0f ? 0.0f : w * exp_of<T>(z - lse);
-        }
+        for (int r = 0; r < 4; ++r)
+          d[r] = w[j] == 0.0f ? 0.0f : w[j] * exp_of<T>(acc[i][j][r] - lse[j]);
         if constexpr (VA == 1) {
           *reinterpret_cast<f4*>(st + l16 * S + 16 * i + 4 * q) = f4{d[0], d[1], d[2], d[3]};
         } else {
@@ -61,12 +112,8 @@ struct SlopeEnd {
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      if (q == 0 && w != 0.0f) {                  // one lane a column: equal classes one after the other
-        for (int e = lo; e < hi; ++e) {
-          const int64_t rel = entry_row(p.y, n, e, p.row0 + m0);
-          if (rel < 0 || rel >= ROWS) continue;
-          st[l16 * S + (int)rel] -= p.y.label ? w : w * p.y.weight[(int64_t)n * p.y.k + e];
-        }
+      if (q == 0 && w[j] != 0.0f) {               // one lane a column: equal classes one after the other
+        entries[j].template each<true>(p.y, n, p.row0 + m0, ROWS, 1, [&](int, int row, float weight) { st[l16 * S + row] -= w[j] * weight; });
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -195,8 +242,10 @@ __global__ __launch_bounds__(256) void row_sum_kernel(int M, int parts, const fl
 
 // Classes of a piece: 8192, or as many as make 128 MB of dZ, which the last-level cache
 // still holds when the products read it.  Multiples of 256 (whole tiles, whole bins).
+constexpr int64_t kPieceRows = 8192, kPieceBytes = 256ll << 20;
+
 int64_t piece_rows(int dtype, int64_t kn, int64_t t) {
-  const int64_t most = std::min<int64_t>(1 << 20, std::max<int64_t>(8192, (128ll << 20) / (std::max<int64_t>(t, 1) * type_size(dtype))));
+  const int64_t most = std::min<int64_t>(1 << 20, std::max<int64_t>(kPieceRows, kPieceBytes / (std::max<int64_t>(t, 1) * type_size(dtype))));
   const int64_t pieces = std::max<int64_t>(1, ceil_div(kn, most));
   return ceil_div(std::max<int64_t>(1, ceil_div(kn, pieces)), 256) * 256;
 }
@@ -210,7 +259,7 @@ struct Backward {
   int64_t lddz = 0;
   Lines x, f, d;                   // as the products find them
   int splits = 1;                  // of dX's partial products (several pieces)
-  int64_t back = 0, lists = 0, xcopy = 0, fcopy = 0, dz = 0, db = 0, dx = 0, product = 0, bytes = 0;
+  int64_t back = 0, lists = 0, xcopy = 0, fcopy = 0, dz = 0, db = 0, dx = 0, shares = 0, product = 0, bytes = 0;
 };
 
 int64_t whole(int dtype, int64_t n) { return std::max<int64_t>(padded(dtype, n), 1); }
@@ -247,12 +296,13 @@ Backward backward_layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_ord
   w.dz = w.fcopy + (w.copy_f ? up256((f_order ? w.ldx * most : w.lddz * ci) * size) : 0);
   w.db = w.dz + up256(w.lddz * t * size);
   int64_t parts = 0;                                        // of dbias: over the pieces' sizes
-  int64_t product = 0;
+  int64_t product = 0, shares = 0;
   const int64_t last = kn - (w.pieces - 1) * w.rows;
   for (int64_t rows : {most, last}) {
     const Lines fl = piece_lines(dtype, f_order, w.copy_f, f, ci, rows);
     const LossPlan l = loss_plan(dtype, f_order == 1, fl, w.x, rows, t, ci);
     parts = std::max(parts, ceil_div(t, l.cols) * rows);
+    shares = std::max(shares, share_bytes(l, rows, t));
     if (want_dx && w.pieces == 1) product = std::max(product, product_workspace(dtype, f_order == 0, true, fl, w.d, ci, t, rows));
     if (want_df)
       product = std::max(product, f_order ? product_workspace(dtype, false, false, w.x, w.d, ci, rows, t)
@@ -264,7 +314,8 @@ Backward backward_layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_ord
     w.splits = product_splits(dtype, f_order == 0, true, w.f, w.d, ci, t, most);
     w.product += up256(w.splits * ci * t * 4);
   }
-  w.bytes = w.product + product;
+  w.shares = w.product;                                     // read before the products that follow
+  w.bytes = w.product + std::max(product, shares);
   return w;
 }
 
@@ -354,6 +405,7 @@ template <class T> hipError_t loss_backward(const LossCall& c, const Wanted& o, 
       p.dZ = dz;
       p.lddz = lddz;
       p.db = o.dbias ? reinterpret_cast<float*>(ws + w.db) : nullptr;
+      p.shares = reinterpret_cast<float*>(ws + w.shares);
       if ((e = launch_loss_typed<SlopeEnd, T>(c.dtype, order == 1, p, nullptr, s)) != hipSuccess) break;
     }
     if (o.dbias && rows > 0) {

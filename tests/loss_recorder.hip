@@ -28,6 +28,11 @@ SHOWN hipError_t hipLaunchKernel(const void* host, dim3 grid, dim3 block, void**
   if (is("column_kernel")) put("t", whole(0)), put("w", arg(6)), put("back", arg(7));
   if (is("input_kernel")) put("t", *static_cast<const int64_t*>(args[1])), put("w", arg(4)), put("to", arg(5)), put("ldto", *static_cast<const int64_t*>(args[6]));
   if (is("row_sum_kernel")) put("M", whole(0)), put("parts", whole(1)), put("part", arg(2));
+  if (is("shared_loss_kernel") || is("shared_dz_kernel")) {
+    const linear::LossProduct& p = *static_cast<const linear::LossProduct*>(args[0]);
+    put("M", p.M), put("N", p.N), put("row0", p.row0), put("shares", p.shares), put("w", p.w), put("dZ", p.dZ), put("lddz", p.lddz);
+    put("db", p.db), put("splits", whole(1));
+  }
   if (is("ring_kernel") || is("wide_kernel")) put("adds", (int64_t)static_cast<const linear::Product*>(args[0])->add);
   text += "}\n";
   return hipSuccess;
