@@ -32,9 +32,10 @@
  * (linear.h); losses, lse and g are fp32.  Z is summed in fp32, and everything up to
  * the loss is computed in fp32.  The gradients compute Z again, a piece of the classes
  * at a time (8192 or more); a piece's dZ is held in the layer's type, one rounding
- * (fp16: times a power of two that puts the largest finite |g| T between 2^14 and
- * 2^15), dX is added up over the pieces in fp32, and each result is rounded once.
- * dbias is summed before that rounding.  Every result is reproducible.
+ * (16-bit types: times a factor that puts the largest finite |g| T at 2^15, so that
+ * neither large nor small g leave fp16's range), dX is added up over the pieces in fp32,
+ * and each result is rounded once: a 16-bit dX or dF is off by up to about 1.4 roundings
+ * in its norm.  dbias is summed before that rounding.  Every result is reproducible.
  *
  * Storage and rules are linear.h's: X and dX have their first index fastest and a
  * leading dimension; F and dF have either index fastest (f_order); any address and

@@ -847,8 +847,8 @@ def linear_cross_entropy_backward(F, X, labels, lse, dloss, bias=None, ignore_in
         dX = F^T dZ,    dF = dZ X^T,    dbias = dZ 1.
 
     Z is computed again, a piece of 8192 classes or more at a time; a piece's dZ is
-    rounded to the layer's type once (fp16: times a power of two), dX is summed over the
-    pieces in float32.  Ignored tokens, and tokens with dloss = 0, add nothing whatever
+    rounded to the layer's type once (16-bit types: times a factor, so that its range does
+    not matter), dX is summed over the pieces in float32.  Ignored tokens, and tokens with dloss = 0, add nothing whatever
     their X holds.  dX is stored like X, dF in F's order; ``needs`` leaves out what is
     not wanted (None is returned in its place)."""
     layer = _loss_layer(F, X, bias)

@@ -178,7 +178,7 @@ struct Epilogue {
   void* C;
   int64_t ldc;
   int act;
-  const float* scale;     // fp16 only: one value (a power of two) or nullptr
+  const float* scale;     // 16-bit types only: one value or nullptr
 };
 
 // C (M x N, M fastest) = A (M x K) B (K x N).
@@ -229,7 +229,7 @@ __device__ inline void finish(const Epilogue& e, int m, int n, int cnt, F sums) 
   if (e.bias) load_part<T, WHOLE>(static_cast<const T*>(e.bias) + m, cnt, b);
   if (e.residual) load_part<T, WHOLE>(static_cast<const T*>(e.residual) + (int64_t)n * e.ldr + m, cnt, r);
   sums(v);
-  if constexpr (std::is_same_v<T, f16>) {
+  if constexpr (sizeof(T) == 2) {
     if (e.scale) {
       const float c = *e.scale;
 #pragma unroll
@@ -251,7 +251,7 @@ __device__ inline void finish(const Epilogue& e, int m, int n, int cnt, F sums) 
 
 // The same for one value.
 template <class T> __device__ inline void finish_one(const Epilogue& e, int m, int n, float v) {
-  if (std::is_same_v<T, f16> && e.scale) v *= *e.scale;
+  if (sizeof(T) == 2 && e.scale) v *= *e.scale;
   if (e.bias) v += (float)static_cast<const T*>(e.bias)[m];
   if (e.Z) static_cast<T*>(e.Z)[(int64_t)n * e.ldz + m] = (T)v;
   act_values<T, 1>(&v, e.act);

@@ -89,7 +89,7 @@ struct LossProduct : Product {
   float* at;
   // gradients
   const float* lse;         // N
-  const float* w;           // N: g T (times fp16's power of two); 0 where nothing counts
+  const float* w;           // N: g T (16-bit types: times a factor for all); 0 where nothing counts
   void* dZ;
   int64_t lddz;             // M rounded up to whole vectors
   float* db;                // [column parts][M] sums of dZ's rows, or nullptr

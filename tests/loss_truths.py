@@ -101,7 +101,7 @@ def forward_bound(F, X, bias, case):
 def backward_bound(F, X, bias, case, g, dtype):
     """Bounds of dX, dF, dbias: p by the errors of its exponent, the weights as above,
     a subtraction and two products; one rounding of dZ to the type (not for dbias;
-    fp16: relative to a power of two, whose lower end loses 2^-39 of the largest g T);
+    16-bit types: times a factor, below which 2^-39 of the largest g T is lost);
     fp32 sums; one rounding of each result."""
     kn, t = F.shape[0], X.shape[1]
     at, q, keep, _, T = targets(case, kn, t, F.device)
@@ -117,7 +117,7 @@ def backward_bound(F, X, bias, case, g, dtype):
     eq = 16 * EPS if "labels" in case else 4 * EPS * (torch.where(top.abs() < torch.inf, top, 0.0)).abs().max() * 2 + (q.shape[0] + 32) * EPS
     e = w * e.scatter_add(0, at, q * eq) + 8 * EPS * (d.abs() + w * p)
     u = UNIT[dtype]
-    held = e + u * (d.abs() + e) + (w.max() * 2.0 ** -39 if dtype == torch.float16 else TINY[dtype])
+    held = e + u * (d.abs() + e) + (TINY[dtype] if dtype == torch.float32 else w.max() * 2.0 ** -39)
     held = torch.where(w == 0, 0.0, held)
     big = d.abs() + held
     Fa, Xa = F.double().abs(), torch.where(w == 0, 0.0, X.double().abs())

@@ -120,7 +120,7 @@ def check_inside(need, call, code, launched):
             write("bin", v["bin"], t * (bins + 1) * 2), write("counts", v["counts"], t * 4)
         elif k == "column_kernel":
             write("w", v["w"], t * 4)
-            if dtype == F16:
+            if dtype != F32:
                 write("back", v["back"], 4)
         elif k == "input_kernel":
             reads("w", v["w"])
