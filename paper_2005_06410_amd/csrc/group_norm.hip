@@ -258,11 +258,15 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
 template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, char* ws, hipStream_t s) {
   if (p.resident) {
     const int64_t floats = p.threads * (int64_t)kHeld<T, MODE> + (int64_t)p.slots * p.unit_groups * p.shares;
-    if (p.threads == 512) return start_resident(norm_resident_kernel<T, 512, 8, MODE>, p, a, floats, s);
-    switch (p.held) {
-      case 1: return start_resident(norm_resident_kernel<T, 256, 1, MODE>, p, a, floats, s);
-      case 4: return start_resident(norm_resident_kernel<T, 256, 4, MODE>, p, a, floats, s);
-      default: return start_resident(norm_resident_kernel<T, 256, 8, MODE>, p, a, floats, s);
+    if constexpr (MODE == kTiny) {
+      return start_resident(norm_resident_kernel<T, 256, 8, MODE>, p, a, floats, s);
+    } else {
+      if (p.threads == 512) return start_resident(norm_resident_kernel<T, 512, 8, MODE>, p, a, floats, s);
+      switch (p.held) {
+        case 1: return start_resident(norm_resident_kernel<T, 256, 1, MODE>, p, a, floats, s);
+        case 4: return start_resident(norm_resident_kernel<T, 256, 4, MODE>, p, a, floats, s);
+        default: return start_resident(norm_resident_kernel<T, 256, 8, MODE>, p, a, floats, s);
+      }
     }
   }
   if (!a.mean) a.mean = reinterpret_cast<float*>(ws + p.stats);

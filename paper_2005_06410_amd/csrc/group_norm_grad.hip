@@ -369,11 +369,15 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
     // group_sums() of two values, or the sums by channel behind the images
     const int64_t floats = std::max(2 * (p.threads * (int64_t)kHeld<T, MODE> + (int64_t)p.slots * p.unit_groups * p.shares),
                                     p.threads * (int64_t)kVec<T>);
-    if (p.threads == 512) return start_resident(norm_resident_grad_kernel<T, 512, 8, MODE>, p, a, floats, s);
-    switch (p.held) {
-      case 1: return start_resident(norm_resident_grad_kernel<T, 256, 1, MODE>, p, a, floats, s);
-      case 4: return start_resident(norm_resident_grad_kernel<T, 256, 4, MODE>, p, a, floats, s);
-      default: return start_resident(norm_resident_grad_kernel<T, 256, 8, MODE>, p, a, floats, s);
+    if constexpr (MODE == kTiny) {
+      return start_resident(norm_resident_grad_kernel<T, 256, 8, MODE>, p, a, floats, s);
+    } else {
+      if (p.threads == 512) return start_resident(norm_resident_grad_kernel<T, 512, 8, MODE>, p, a, floats, s);
+      switch (p.held) {
+        case 1: return start_resident(norm_resident_grad_kernel<T, 256, 1, MODE>, p, a, floats, s);
+        case 4: return start_resident(norm_resident_grad_kernel<T, 256, 4, MODE>, p, a, floats, s);
+        default: return start_resident(norm_resident_grad_kernel<T, 256, 8, MODE>, p, a, floats, s);
+      }
     }
   }
   a.parts = a.b * p.chunks;
