@@ -1,9 +1,10 @@
 """Trains the fully connected head of a small convolutional network with the
-library's operators together: one CONVGEMM layer makes the features, two
-``linear`` layers (GELU and a residual in the first, classes in the second) make
-the scores, ``linear_backward`` their gradients, and ``clip_grad_norm`` bounds
-the step.  Images and labels are synthetic: each class has a pattern of its own,
-and the images are noisy copies.
+library's operators together: one CONVGEMM layer and its ``group_norm`` make the
+features, two ``linear`` layers (GELU, SiLU and a residual) come before the classes,
+whose scores ``linear_cross_entropy`` never writes; its gradients and
+``linear_backward`` lead back, and ``clip_grad_norm`` bounds the step.  Images and
+labels are synthetic: each class has a pattern of its own, and the images are noisy
+copies.
 
     python examples/train_head.py [--steps 60] [--dtype bf16|f16|f32]
 """
@@ -28,10 +29,12 @@ def leftmost_fastest(shape, gen, scale):
 
 
 def features(images, filters):
-    """(ci, batch) features: one convolution with stride 2, relu, flattened."""
+    """(ci, batch) features: one convolution with stride 2, normalised in groups of
+    four channels, relu, flattened."""
     o = lt.convgemm(filters, images, stride=2)            # (kn, ho, wo, batch), leftmost fastest
     kn, ho, wo, b = o.shape
-    return o.as_strided((kn * ho * wo, b), (1, kn * ho * wo)).clamp_min(0)
+    o, _, _ = lt.group_norm(o, kn // 4, activation="relu", out=o)
+    return o.as_strided((kn * ho * wo, b), (1, kn * ho * wo))
 
 
 def train(steps=60, dtype="bf16", classes=10, batch=64, hidden=256, rate=0.5, max_norm=1.0, seed=0):
@@ -47,6 +50,7 @@ def train(steps=60, dtype="bf16", classes=10, batch=64, hidden=256, rate=0.5, ma
     master = [torch.randn(hidden, ci, generator=gen, device="cuda") * ci ** -0.5, torch.zeros(hidden, device="cuda"),
               torch.randn(hidden, hidden, generator=gen, device="cuda") * hidden ** -0.5, torch.zeros(hidden, device="cuda"),
               torch.randn(classes, hidden, generator=gen, device="cuda") * hidden ** -0.5, torch.zeros(classes, device="cuda")]
+    mean = torch.full((), 1.0 / batch, device="cuda")                    # dL/dloss of every image
     losses, norms = [], []
     for _ in range(steps):
         label = torch.randint(0, classes, (batch,), generator=gen, device="cuda")
@@ -55,12 +59,9 @@ def train(steps=60, dtype="bf16", classes=10, batch=64, hidden=256, rate=0.5, ma
         F1, b1, F2, b2, F3, b3 = (p.to(d) for p in master)
         h1, z1 = lt.linear(F1, x, bias=b1, activation="gelu", keep_pre=True)
         h2, z2 = lt.linear(F2, h1, bias=b2, activation="silu", residual=h1, keep_pre=True)
-        scores = lt.linear(F3, h2, bias=b3).float()                     # (classes, batch)
-        p = torch.softmax(scores, dim=0)
-        losses.append(-torch.log(p.gather(0, label[None, :]) + 1e-30).mean())
-        p.scatter_add_(0, label[None, :], torch.full((1, batch), -1.0, device="cuda"))
-        ds = (p / batch).t().contiguous().t().to(d)                     # dL/dscores
-        dh2, dF3, db3 = lt.linear_backward(F3, h2, ds)
+        loss, lse = lt.linear_cross_entropy(F3, h2, label, bias=b3)
+        losses.append(loss.mean())
+        dh2, dF3, db3 = lt.linear_cross_entropy_backward(F3, h2, label, lse, mean, bias=b3)
         dh1, dF2, db2 = lt.linear_backward(F2, h1, dh2, pre=z2, activation="silu")
         _, dF1, db1 = lt.linear_backward(F1, x, dh1 + dh2, pre=z1, activation="gelu", needs=(False, True, True))
         grads = [dF1, db1, dF2, db2, dF3, db3]

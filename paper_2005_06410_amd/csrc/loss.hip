@@ -300,8 +300,13 @@ Forward forward_layout(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order
   return w;
 }
 
-int loss_forward(const LossCall& c, float* loss, float* lse, char* ws, hipStream_t s) {
-  if (c.t == 0) return LINEAR_OK;
+// Columns of one round: all of them, but for so many logits that a launch would hold more
+// threads than 32 bits count, or the parts of the columns more memory than the operands.
+int64_t round_columns(int64_t kn, int64_t t) {
+  return kn * t <= 1ll << 33 ? t : std::max<int64_t>(4096, (1ll << 33) / kn / 256 * 256);
+}
+
+int forward_round(const LossCall& c, float* loss, float* lse, char* ws, hipStream_t s) {
   const Lines f = lines_of(c.dtype, c.F, c.ldf, c.f_order ? c.ci : c.kn), x = lines_of(c.dtype, c.X, c.ldx, c.ci);
   const Forward w = forward_layout(c.dtype, c.kn, c.ci, c.t, c.f_order, c.k, f, x);
   LossProduct p{};
@@ -344,9 +349,31 @@ int loss_forward(const LossCall& c, float* loss, float* lse, char* ws, hipStream
   return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
 }
 
+int loss_forward(const LossCall& all, float* loss, float* lse, char* ws, hipStream_t s) {
+  const int64_t step = round_columns(all.kn, all.t), size = type_size(all.dtype), isize = all.itype == LOSS_I64 ? 8 : 4;
+  auto ahead = [](const void* p, int64_t bytes) { return p ? static_cast<const void*>(static_cast<const char*>(p) + bytes) : p; };
+  for (int64_t n = 0; n < all.t; n += step) {
+    LossCall c = all;
+    c.t = std::min(step, all.t - n);
+    c.X = ahead(all.X, n * all.ldx * size);
+    c.labels = ahead(all.labels, n * isize);
+    c.top = ahead(all.top, all.k ? n * all.ldtop * type_size(all.ttype) : 0);
+    c.index = ahead(all.index, n * all.ldi * isize);
+    if (int e = forward_round(c, loss + n, lse + n, ws, s)) return e;
+  }
+  return LINEAR_OK;
+}
+
+// The bytes for all rounds: the last one has fewer columns, and with them another plan.
+int64_t forward_bytes(int dtype, int64_t kn, int64_t ci, int64_t t, int f_order, int k, Lines f, Lines x) {
+  const int64_t step = round_columns(kn, t), last = t > step ? (t - 1) % step + 1 : step;
+  return std::max(forward_layout(dtype, kn, ci, step, f_order, k, f, x).bytes, forward_layout(dtype, kn, ci, last, f_order, k, f, x).bytes);
+}
+
+// Every round's X has the first one's lines: they begin whole leading dimensions apart.
 int64_t need_of(const LossCall& c) {
-  return forward_layout(c.dtype, c.kn, c.ci, c.t, c.f_order, c.k, lines_of(c.dtype, c.F, c.ldf, c.f_order ? c.ci : c.kn),
-                        lines_of(c.dtype, c.X, c.ldx, c.ci)).bytes;
+  return forward_bytes(c.dtype, c.kn, c.ci, c.t, c.f_order, c.k, lines_of(c.dtype, c.F, c.ldf, c.f_order ? c.ci : c.kn),
+                       lines_of(c.dtype, c.X, c.ldx, c.ci));
 }
 
 }  // namespace
@@ -371,7 +398,7 @@ int check_teacher(const LossCall& c) {
   if (c.itype != LOSS_I32 && c.itype != LOSS_I64) return -16;
   if (bad_ld(c.ldi, c.k)) return -17;
   if (!(c.temperature > 0) || !std::isfinite((float)c.temperature) || !std::isfinite((float)(1.0 / c.temperature)) ||
-      !std::isfinite((float)(c.temperature * c.temperature)))
+      !std::isnormal((float)(c.temperature * c.temperature)))
     return -18;
   return 0;
 }
@@ -414,10 +441,10 @@ extern "C" int64_t convgemm_linear_loss_workspace(int dtype, int64_t kn, int64_t
   if (k < 0 || k > LOSS_MAX_K || t * k >= kElemLimit) return -6;
   if (t == 0) return 0;
   if (aligned)
-    return forward_layout(dtype, kn, ci, t, f_order, k, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci)).bytes;
+    return forward_bytes(dtype, kn, ci, t, f_order, k, lines_if(dtype, true, f_order ? ci : kn), lines_if(dtype, true, ci));
   int64_t most = 0;
   for (Lines f : kAnyLines)
-    for (Lines x : kAnyLines) most = std::max(most, forward_layout(dtype, kn, ci, t, f_order, k, f, x).bytes);
+    for (Lines x : kAnyLines) most = std::max(most, forward_bytes(dtype, kn, ci, t, f_order, k, f, x));
   return most;
 }
 

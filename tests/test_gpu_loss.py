@@ -128,6 +128,37 @@ def test_strides_and_addresses(dtype, order, pad, shift):
         check(F, X, b, {"labels": labels_of(g, kn, t), "ignore": IGNORE}, gradient_of(g, t))
 
 
+def test_views_of_a_teacher():
+    """Leading dimensions of the teacher's logits and classes beyond k, each its own."""
+    g = gen(22)
+    F, X, b = layer(g, 700, 40, 50, torch.bfloat16, 1)
+    top, index = teacher_of(g, 700, 50, 9, torch.float32)
+    wide_top, wide_index = torch.full((50, 13), 1e4, device="cuda"), torch.full((50, 16), 3, dtype=torch.int32, device="cuda")
+    wide_top[:, 2:11], wide_index[:, 5:14] = top.t(), index.t().int()
+    want = lt().linear_distill(F, X, top, index, bias=b)
+    got = lt().linear_distill(F, X, wide_top[:, 2:11].t(), wide_index[:, 5:14].t(), bias=b)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    one = torch.ones((), device="cuda")
+    for a, v in zip(lt().linear_distill_backward(F, X, wide_top[:, 2:11].t(), wide_index[:, 5:14].t(), want[1], one, bias=b),
+                    lt().linear_distill_backward(F, X, top, index, want[1], one, bias=b)):
+        assert torch.equal(a, v)
+
+
+def test_more_logits_than_one_round():
+    """2^33 logits and more are taken in rounds of columns: the columns on both sides of a
+    border, and the last ones, as from a call of their own."""
+    g = gen(23)
+    kn, t = 131072, 70000                            # rounds of 65536 columns
+    F = (torch.randn(kn, 16, generator=g, device="cuda") * 0.5).bfloat16()
+    X = torch.randn(t, 16, generator=g, device="cuda").bfloat16().t()
+    y = labels_of(g, kn, t)
+    loss, lse = lt().linear_cross_entropy(F, X, y)
+    for a, b in [(0, 300), (65436, 65636), (t - 200, t)]:
+        case = {"labels": y[a:b], "ignore": IGNORE}
+        for got, want, bound in zip((loss[a:b], lse[a:b]), truth.forward(F, X[:, a:b], None, case), truth.forward_bound(F, X[:, a:b], None, case)):
+            within(got, want, bound, "a round")
+
+
 @pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_several_pieces(dtype, order):

@@ -98,6 +98,7 @@ def check_inside(need, call, code, launched):
     dtype, kn, ci, t, _, order = args[:6]
     size, back = SIZE[dtype], "backward" in name
     assert code == 0, (call, code)
+    columns = 0
     live = {}                                        # what later launches read: name -> (address, bytes)
 
     def write(what, at, n, over=()):
@@ -115,9 +116,10 @@ def check_inside(need, call, code, launched):
         assert v["grid"] * v["block"] < 1 << 32
         if k == "list_kernel":
             bins = -(-kn // 128)
-            assert v["bins"] == bins and v["size"] >= v["k"] and v["size"] <= 1024 and v["grid"] == t
-            write("sorted", v["sorted"], t * v["k"] * 4), write("weight", v["weight"], t * v["k"] * 4)
-            write("bin", v["bin"], t * (bins + 1) * 2), write("counts", v["counts"], t * 4)
+            n = v["grid"]
+            assert v["bins"] == bins and v["size"] >= v["k"] and v["size"] <= 1024 and (n == t or not back)
+            write("sorted", v["sorted"], n * v["k"] * 4), write("weight", v["weight"], n * v["k"] * 4)
+            write("bin", v["bin"], n * (bins + 1) * 2), write("counts", v["counts"], n * 4)
         elif k == "column_kernel":
             write("w", v["w"], t * 4)
             if dtype != F32:
@@ -133,7 +135,10 @@ def check_inside(need, call, code, launched):
                 write(what, v[c + "to"], v[c + "lines"] * v[c + "to_ld"] * size, over=("copya_", "copyb_"))
         elif k in ("loss_ring_kernel", "loss_wide_kernel"):
             rows, cols = tile_of(v)
-            assert v["splits"] == 1 and v["part"] == 0 and v["row0"] % 256 == 0 and v["row0"] + v["M"] <= kn and v["N"] == t
+            assert v["splits"] == 1 and v["part"] == 0 and v["row0"] % 256 == 0 and v["row0"] + v["M"] <= kn
+            n = v["N"]
+            assert n == t if back else n <= t
+            columns += 0 if back else n
             for operand in (v["A"], v["B"]):
                 assert operand >= F or operand == 0 or any(a == operand for a, _ in live.values()) or ci == 0
             if v["k"]:
@@ -146,10 +151,11 @@ def check_inside(need, call, code, launched):
                 if v["db"]:
                     write("dbpart", v["db"], -(-t // cols) * v["M"] * 4)
             else:
-                write("sums", v["sums"], -(-v["M"] // rows) * t * 8), write("at", v["at"], t * max(v["k"], 1) * 4)
+                write("sums", v["sums"], -(-v["M"] // rows) * n * 8), write("at", v["at"], n * max(v["k"], 1) * 4)
         elif k in ("shared_loss_kernel", "shared_dz_kernel"):
             reads("part", v["shares"], v["splits"] * v["M"] * v["N"] * 4)
             assert v["N"] == t and v["row0"] + v["M"] <= kn
+            columns += 0 if back else t
             if back:
                 reads("w", v["w"])
                 assert v["lddz"] >= v["M"] and v["lddz"] * size % 16 == 0
@@ -160,8 +166,9 @@ def check_inside(need, call, code, launched):
             live.pop("part")
         elif k == "join_loss_kernel":
             if kn:
-                reads("sums", v["sums"], v["parts"] * t * 8), reads("at", v["at"])
-                assert live["sums"][1] == v["parts"] * t * 8
+                reads("sums", v["sums"], v["parts"] * v["N"] * 8), reads("at", v["at"])
+                assert live["sums"][1] == v["parts"] * v["N"] * 8
+            live.clear()                              # the next round of columns starts over
         elif k == "row_sum_kernel":
             if t:
                 reads("dbpart", v["part"], v["parts"] * v["M"] * 4)
@@ -177,6 +184,7 @@ def check_inside(need, call, code, launched):
                 live.pop("copya_", None), live.pop("copyb_", None), live.pop("part", None)
         else:
             assert k == "join_kernel", v
+    assert back or columns == t or kn == 0
     if back and args[-8] is not None and kn * ci * t:      # dX: every class contributes once
         done = [v for v in launched if kind(v) in ("ring_kernel", "wide_kernel") and DX <= v["C"] < DF]
         assert sum(v["K"] for v in done) == kn
@@ -213,6 +221,8 @@ def test_everything_stays_inside(lib, recorder, dtype, monkeypatch):
 def test_long_lines_and_empty_extents_stay_inside(lib, recorder, dtype, monkeypatch):
     calls = []
     sizes = [(a, b, c) for long in EDGES for a, b, c in [(long, 64, 80), (long, 16, 3), (16, long, 5), (1000, long, 80), (200, 24, long)]]
+    # more logits than one round holds
+    sizes += [(1 << 18, 16, 1 << 21), (131073, 24, (1 << 20) + 7), (LIMIT - 1, 8, 65535), (3, 5, LIMIT - 1)]
     sizes += [(0, 5, 5), (5, 0, 5), (5, 5, 0), (0, 0, 3), (1, 1, 1)]
     for kn, ci, t in sizes:
         for order in (0, 1):
@@ -259,7 +269,7 @@ LAYER_FAULTS = [({"dtype": 0}, -1), ({"kn": -1}, -2), ({"kn": LIMIT}, -2), ({"ci
                 ({"order": 2}, -6), ({"ldf": 3}, -7), ({"X": None}, -8), ({"ldx": 2}, -9)]
 LABEL_FAULTS = [({"labels": None}, -11), ({"itype": 3}, -12)]
 TEACHER_FAULTS = [({"k": 0}, -11), ({"k": 1025}, -11), ({"top": None}, -12), ({"ttype": 2}, -13), ({"ldtop": 1}, -14), ({"index": None}, -15), ({"itype": 0}, -16),
-                  ({"ldi": 1}, -17), ({"temperature": 0.0}, -18), ({"temperature": float("nan")}, -18), ({"temperature": 1e300}, -18), ({"temperature": 1e-45}, -18)]
+                  ({"ldi": 1}, -17), ({"temperature": 0.0}, -18), ({"temperature": float("nan")}, -18), ({"temperature": 1e300}, -18), ({"temperature": 1e-45}, -18), ({"temperature": 1e-30}, -18)]
 
 
 def faults(first):
