@@ -3,6 +3,17 @@
 // What a thread owns is always one 16-byte vector of channels (V = 4 or 8), at every
 // `rows`-th position: neighbouring threads take neighbouring vectors, so that loads are
 // whole lines, and sums by channel stay in one thread's registers until the end.
+//
+// All of it is bound by memory, and by latencies where there is little (a kernel of this
+// kind takes 4 to 5 us at least).  Three ways:
+// * features (one position an image): a group in the lanes of a wave, no barriers.  4001
+//   tokens of 1000 channels bf16, GELU: 12 us, gradients 14 (through LDS: 23 and 34).
+// * resident: a unit of whole groups in a workgroup's registers, one read and one write.  27 x
+//   27 x 256 x 80 fp32, 32 groups: 26 us (4.6 TB/s), gradients 40 (4.5 TB/s).
+// * split, for larger maps: two reads.  256 x 256 x 128 x 16 bf16: 49 us for the statistics
+//   (5.5 TB/s), 92 for the result (5.9), 101 and 137 for the gradients (5.3 and 5.9).  Rounds of
+//   images that the last-level cache could hold from the first pass to the second were no
+//   faster (162 us instead of 146 forward): the second read is not what bounds it, and each round adds three launches.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -412,7 +423,8 @@ inline NormPlan plan_of(int dtype, int64_t c, int64_t s, int64_t b, int64_t grou
     p.bytes = grad ? up(2 * (int64_t)p.blocks * c * 4) : 0;
     return p;
   }
-  // resident: 0.2 (0.4) ns a value of one workgroup on a compute unit
+  // resident: 0.2 (0.4) ns a value of one workgroup on a compute unit, and 5 us; split: the
+  // same spread over all units, and what its three (four) launches take
   const double each = (double)unit * V * s * (grad ? 0.4e-3 : 0.2e-3), rounds = (double)div_up(div_up(all, unit) * b, cu);
   const double split = (grad ? 28.0 : 18.0) + each * div_up(all, unit) * b / cu;
   if (fits(unit, p.mode == kTiny ? 256 : 512) && 5.0 + each * rounds <= split) {

@@ -1,6 +1,9 @@
 // Losses over a layer's outputs, gradients: for one piece of the classes after the
 // other, Z = F X + bias again with dZ = w (p - q) in the product's epilogue, then
 // dF = dZ X^T of the piece and its share of dX = F^T dZ, which is added up in fp32.
+//
+// Bound by the three products: a piece of 16384 classes of 4096 features by 8192 tokens bf16
+// takes 843 us with dZ, 893 for dF and 862 for dX (1300, 1230 and 1280 TFLOP/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -53,7 +56,8 @@ template <class T> __global__ __launch_bounds__(256) void shared_dz_kernel(LossP
 }
 
 // Ends a wave's tile with dZ, and with the sums of its rows for dbias.  A column whose
-// w is 0 is written as zeros, whatever Z is there.
+// w is 0 is written as zeros, whatever Z is there.  dZ goes through LDS, 16 columns at a
+// time, so that it is stored as whole vectors; there the targets' weights are taken off.
 struct SlopeEnd {
   using P = LossProduct;
   template <class T> static hipError_t from_shares(const P& p, int splits, hipStream_t s) {
@@ -242,8 +246,11 @@ __global__ __launch_bounds__(256) void row_sum_kernel(int M, int parts, const fl
   dbias[m] = (T)s;
 }
 
-// Classes of a piece: 8192, or as many as make 128 MB of dZ, which the last-level cache
-// still holds when the products read it.  Multiples of 256 (whole tiles, whole bins).
+// Classes of a piece: 8192, or as many as make 256 MB of dZ.  A piece adds its share of dX
+// to memory and starts four launches; dZ is a piece's workspace.  131072 classes by 8192
+// tokens bf16, loss and gradients: 27.8 ms with 4096 classes a piece, 26.6 with 8192, 26.2
+// with 16384 (256 MB), 26.1 with 32768, 25.9 with 65536 (1 GB, half of what the logits would
+// take).  Multiples of 256 (whole tiles, whole bins).
 constexpr int64_t kPieceRows = 8192, kPieceBytes = 256ll << 20;
 
 int64_t piece_rows(int dtype, int64_t kn, int64_t t) {
