@@ -23,7 +23,7 @@
  *
  * g_n = dL/dloss_n; gradients: dX = F^T dZ, dF = dZ X^T, dbias = dZ 1.  A column with
  * g_n = 0, or one that does not count, adds nothing to dF and dbias even where X or Z
- * are infinite or NaN there, and its dX is zero.
+ * are infinite or NaN there or its target is invalid, and its dX is zero.
  *
  * Classes can be masked by a bias of -infinity: p is 0 there.  A column in which every
  * class is masked has lse = -infinity and NaN gradients.

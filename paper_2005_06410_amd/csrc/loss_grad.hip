@@ -172,6 +172,7 @@ __global__ __launch_bounds__(1024) void column_kernel(int t, int64_t kn, const f
                                                       Targets y, float* __restrict__ w, float* __restrict__ back) {
   auto value = [&](int n) {
     const float v = g[(int64_t)n * ginc] * temperature;
+    if (v == 0.0f) return 0.0f;
     if (y.label) {
       const int64_t label = label_of(y, n);
       return label == y.ignore ? 0.0f : label < 0 || label >= kn ? NAN : v;

@@ -237,6 +237,10 @@ def test_columns_that_do_not_count(dtype):
         dX, dF, db = backward(F, X, b, {"labels": y2, "ignore": IGNORE}, lse, gradient_of(g, t))
         assert dX[:, 7].isnan().all() and dX[:, :7].isfinite().all() and dX[:, 8:].isfinite().all()
         assert dF.isnan().all() and db.isnan().all()
+        without = gradient_of(g, t)
+        without[7] = 0.0
+        for v in backward(F, X, b, {"labels": y2, "ignore": IGNORE}, lse, without):
+            assert v.isfinite().all()
     # every column ignored: zeros, also where X is NaN
     none = {"labels": torch.full((t,), IGNORE, device="cuda"), "ignore": IGNORE}
     loss, lse = forward(F, Xn, b, none)
