@@ -156,28 +156,31 @@ struct StatsEnd {
 // Joins the parts of C columns a workgroup, 256 / C lanes for each, in a fixed order:
 //   lse = base + log sum exp(top_r - base) sum_r,
 // then the loss.  Bound by latency: 18 us for 1024 parts of 8192 columns (67 MB), 4.6 for
-// 500 of one; eight parts under way in each lane (one after the other: 42), and few columns a workgroup where there
-// are few at all (300 columns of 782 parts: 6.9 us by 4, 16.5 by 16).
+// 500 of one; eight parts under way in each lane (one after the other: 42 us), and few
+// columns a workgroup where there are few at all (300 columns of 782 parts by 4: 5.8 us; by
+// 16 more than twice as long).
 template <int C>
 __global__ __launch_bounds__(256) void join_loss_kernel(int parts, int N, int64_t kn, const float2* __restrict__ sums,
                                                         const float* __restrict__ at, Targets y, float temperature2,
                                                         float* __restrict__ loss, float* __restrict__ lse) {
   constexpr int LANES = 256 / C, AHEAD = 8;
-  __shared__ float sh[LANES][C];
-  const int c = threadIdx.x % C, x = threadIdx.x / C, n = blockIdx.x * C + c;
+  __shared__ float sh[2][4][C];
+  const int c = threadIdx.x % C, x = threadIdx.x / C, n = blockIdx.x * C + c, wave = threadIdx.x >> 6;
   const bool there = n < N;
-  auto over = [&](float v, auto f) {
-    sh[x][c] = v;
-    __syncthreads();
+  // over a column's lanes, C apart; `at` is another place in LDS than the call before
+  auto over = [&](float v, int at, auto f) {
 #pragma unroll
-    for (int d = LANES / 2; d > 0; d >>= 1) {
-      if (x < d) sh[x][c] = f(sh[x][c], sh[x + d][c]);
-      __syncthreads();
-    }
-    v = sh[0][c];
+    for (int d = C; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
+    if ((threadIdx.x & 63) < C) sh[at][wave][c] = v;
     __syncthreads();
-    return v;
+    return f(f(sh[at][0][c], sh[at][1][c]), f(sh[at][2][c], sh[at][3][c]));
   };
+  // what the loss needs besides, asked for before the parts
+  const int64_t label = y.label && there ? label_of(y, n) : -1;
+  const int count = !y.label && there ? y.count[n] : 0;
+  const int64_t entry = (int64_t)n * y.k + x;
+  const float own = y.label ? (label >= 0 && label < kn ? at[n] : NAN) : x < count ? at[entry] : 0.0f;
+  const float own_weight = x < count ? y.weight[entry] : 0.0f;
   const float2* s = sums + min(n, N - 1);
   float top = -INFINITY, sum = 0.0f;               // of this lane: sum is relative to top
   for (int r0 = x; r0 < parts; r0 += AHEAD * LANES) {
@@ -196,24 +199,24 @@ __global__ __launch_bounds__(256) void join_loss_kernel(int parts, int N, int64_
     for (int k = 0; k < AHEAD; ++k) sum += v[k].x == -INFINITY ? v[k].y : v[k].y * expf(base_of(v[k].x) - base_of(t));
     top = t;
   }
-  const float all = over(top, [](float a, float b) { return fmaxf(a, b); });
-  sum = over(top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(all)), [](float a, float b) { return a + b; });
+  const float all = over(top, 0, [](float a, float b) { return fmaxf(a, b); });
+  sum = over(top == -INFINITY ? sum : sum * expf(base_of(top) - base_of(all)), 1, [](float a, float b) { return a + b; });
   const float l = base_of(all) + logf(sum);
   if (y.label) {
     if (!there || x > 0) return;
-    const int64_t label = label_of(y, n);
     lse[n] = l;
-    loss[n] = label == y.ignore ? 0.0f : label >= 0 && label < kn ? l - at[n] : NAN;
+    loss[n] = label == y.ignore ? 0.0f : l - own;
     return;
   }
-  const int count = there ? y.count[n] : 0;
-  float v = 0.0f;
+  float v = 0.0f, w = own_weight, z = own;
   for (int e = x; e < count; e += LANES) {
-    const int64_t i = (int64_t)n * y.k + e;
-    const float w = y.weight[i];
-    v += w == 0.0f ? 0.0f : w * (logf(w) - (at[i] - l));
+    if (e > x) {
+      w = y.weight[entry + e - x];
+      z = at[entry + e - x];
+    }
+    v += w == 0.0f ? 0.0f : w * (logf(w) - (z - l));
   }
-  v = over(v, [](float a, float b) { return a + b; });
+  v = over(v, 0, [](float a, float b) { return a + b; });
   if (!there || x > 0) return;
   lse[n] = l;
   loss[n] = count < 0 ? NAN : count == 0 ? 0.0f : temperature2 * v;

@@ -183,6 +183,7 @@ __global__ __launch_bounds__(1024) void column_kernel(int t, int64_t kn, const f
   if constexpr (SCALED) {
     __shared__ float sh[16];
     float top = 0.0f;
+#pragma unroll 4
     for (int n = threadIdx.x; n < t; n += 1024) {
       const float v = fabsf(value(n));
       top = fmaxf(top, v < INFINITY ? v : 0.0f);
@@ -196,6 +197,7 @@ __global__ __launch_bounds__(1024) void column_kernel(int t, int64_t kn, const f
     if (top > 0.0f) scale = 32768.0f / fmaxf(top, 1e-33f);
     if (threadIdx.x == 0) *back = 1.0f / scale;
   }
+#pragma unroll 4
   for (int64_t n = (int64_t)blockIdx.x * 1024 + threadIdx.x; n < t; n += (int64_t)gridDim.x * 1024)
     w[n] = value((int)n) * scale;
 }

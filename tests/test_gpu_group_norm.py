@@ -77,7 +77,7 @@ def affine(g, c, dtype):
 SIZES = [((1, 1), 1), ((6, 5, 3), 2), ((3, 7, 5, 2), 3), ((90, 9, 5, 7), 9), ((64, 13, 13, 3), 32), ((384, 13, 13, 1), 32), ((256, 27, 27, 4), 32),
          ((1000, 41), 8), ((40, 4, 4, 65), 4), ((128, 64, 64, 2), 32), ((24, 300, 2), 1), ((12, 150, 150, 1), 4), ((7, 20011, 2), 7),
          ((1, 70001, 1), 1), ((2048, 2, 3, 5), 1), ((9000, 3, 2), 3), ((4100, 30, 2), 2), ((20000, 1, 3), 1), ((520, 1, 700), 65), ((16, 40000, 3), 16), ((3, 5000), 1), ((4, 3001), 2),
-         ((264, 999), 3), ((4096, 70), 2), ((530, 33), 5)]
+         ((264, 999), 3), ((4096, 70), 2), ((530, 33), 5), ((1024, 77), 1)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -161,6 +161,31 @@ def test_more_logits_than_one_round():
 
 @pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_millions_of_features(dtype, order):
+    """Lines beyond what the direct loads reach go through registers.  X is zero but for 64
+    features, the first and the last among them, so that the same loss follows from these,
+    and the gradients of these and of 64 others."""
+    g = gen(24)
+    ci = (1 << 22) + 8 if dtype == torch.float32 else (1 << 23) + 16
+    kn = 24
+    F, _, b = layer(g, kn, ci, 1, dtype, order, spread=0.3 * ci ** 0.5)
+    at = torch.cat([torch.tensor([0, ci - 1], device="cuda"), torch.randperm(ci - 2, generator=g, device="cuda")[:126] + 1])
+    for t in (5, 20, 80):
+        X = torch.zeros(t, ci, dtype=dtype, device="cuda").t()
+        X[at[:64]] = torch.randn(64, t, generator=g, device="cuda").to(dtype)
+        case, gr = {"labels": labels_of(g, kn, t), "ignore": IGNORE}, gradient_of(g, t)
+        f, x = F[:, at], X[at]
+        loss, lse = forward(F, X, b, case)
+        for got, want, bound in zip((loss, lse), truth.forward(f, x, b, case), truth.forward_bound(f, x, b, case)):
+            within(got, want, bound, "features")
+        dX, dF, db = backward(F, X, b, case, lse, gr)
+        for got, want, bound in zip((dX[at], dF[:, at], db), truth.backward(f, x, b, case, gr), truth.backward_bound(f, x, b, case, gr, dtype)):
+            within(got, want, bound, "features")
+        assert int((dF != 0).any(0).sum()) <= 64
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_several_pieces(dtype, order):
     """More classes than a piece of the gradients holds, the last piece ragged (order 1)
     or a few classes long; entries of a teacher on both sides of each border."""

@@ -236,28 +236,35 @@ def test_long_lines_and_empty_extents_stay_inside(lib, recorder, dtype, monkeypa
 
 
 @needs_hipcc
-def test_the_gpu_tests_reach_every_kernel(lib, recorder, monkeypatch):
-    """Every kernel that the library holds for a loss's product is launched by some size
-    below 2^14 here, and nearly all by the sizes of the GPU tests."""
-    seen = set()
+def test_every_kernel_is_reached(lib, recorder, monkeypatch):
+    """Both ends exist for the tiles and loads that the layer's own products have with a
+    contiguous contraction on the right, and sizes reach all of them."""
     rng = random.Random(7)
-    calls = []
+    seen = {}
     for dtype in (F32, BF16, F16):
+        calls = []
         for order in (0, 1):
-            for _ in range(400):
-                kn, ci, t = int(2 ** rng.uniform(0, 15)), int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 13))
-                if rng.random() < 0.7:
+            for _ in range(700):
+                kn, ci, t = int(2 ** rng.uniform(0, 17)), int(2 ** rng.uniform(0, 13)), int(2 ** rng.uniform(0, 14))
+                if rng.random() < 0.75:
                     kn, ci = up(kn, 8), up(ci, 8)
-                calls += [forward(lib, dtype, kn, ci, t, order), backward(lib, dtype, kn, ci, t, order)]
-    for code, launched in record(recorder, [c for _, c in calls], monkeypatch):
-        assert code == 0
-        seen |= {v["kernel"] for v in launched if kind(v).startswith("loss_")}
-    print(len(seen))
-    out = subprocess.run(["nm", "-C", "--defined-only", lt.LIB_PATH], capture_output=True, text=True).stdout
-    have = {m for m in re.findall(r"loss_(?:ring|wide)_kernel<[^(]*>", out)}
-    short = {re.sub(r"linear::\(anonymous namespace\)::", "", h).replace("DF16b", "unsigned short") for h in have}
-    if short:
-        assert len(seen) <= len(short)
+                calls += [forward(lib, dtype, kn, ci, t, order)[1], backward(lib, dtype, kn, ci, t, order)[1]]
+            for t in (5, 20, 80):
+                calls += [forward(lib, dtype, 24, (1 << 23) + 16, t, order)[1], backward(lib, dtype, 24, (1 << 23) + 16, t, order)[1]]
+        for code, launched in record(recorder, calls, monkeypatch):
+            assert code == 0
+            for v in launched:
+                if kind(v).startswith("loss_"):
+                    seen.setdefault(v["kernel"].replace("linear::", ""), v)
+    rings = {re.search(r"(\w+End), .*Ring<([\w ]+), (\w+), \w+, ([\d, ]+)>", k).groups() for k in seen if "ring" in k}
+    for end in ("StatsEnd", "SlopeEnd"):
+        for kind_ in ("float", "short", "unsigned short"):
+            for kc in ("true", "false"):
+                mine = {r[3] for r in rings if r[:3] == (end, kind_, kc)}
+                # eight tiles for any type, one for a contiguous contraction, two for fp32, three through registers
+                want = 8 + (kc == "true") + 2 * (kind_ == "float") + 3
+                assert len(mine) >= want, (end, kind_, kc, sorted(mine))
+    assert sum("loss_wide_kernel" in k for k in seen) == 8
 
 
 GOOD = dict(dtype=F32, kn=4, ci=3, t=2, F=16, order=0, ldf=4, X=16, ldx=3, bias=None)
