@@ -269,6 +269,27 @@ def test_workspace_is_not_left():
             assert (buffer[:256] == 77).all() and (buffer[256 + need:] == 77).all()
 
 
+def test_maps_beyond_32_bit_offsets():
+    """More than 2^31 values, in one image and over images: rows of 1 and -1 in turn have
+    the mean 0 (or 1 / s of a row) and the variance 1."""
+    for c, s, b in [(256, (1 << 23) + 4, 1), (64, 1 << 20, 34)]:
+        sign = (torch.arange(s, device="cuda", dtype=torch.int32) % 2 * 2 - 1).to(torch.bfloat16)
+        x = sign[:, None].expand(b, s, c).contiguous().permute(2, 1, 0)
+        assert x.numel() > 1 << 31
+        o, mean, rstd = lt().group_norm(x, 8, eps=3.0)
+        assert (mean.abs() < 1e-6).all() and ((rstd - 0.5).abs() < 1e-6).all()
+        for p in (slice(0, 1000), slice(s - 1000, s)):
+            assert torch.equal(o[:, p, b - 1], x[:, p, b - 1] / 2)
+        del o
+        # dO of ones: d - avg d = 0, and xhat has no part in it
+        one = torch.ones((), dtype=torch.bfloat16, device="cuda").expand(b, s, c).contiguous().permute(2, 1, 0)
+        dI, dw, db = lt().group_norm_backward(x, one, 8, mean, rstd)
+        for p in (slice(0, 1000), slice(s - 1000, s)):
+            assert (dI[:, p, b - 1].float().abs() < 1e-6).all()
+        assert ((db.float() - b * s).abs() <= 2.0 ** -8 * b * s).all()
+        del x, one, dI
+
+
 def test_streams_graphs_and_repeats():
     g = gen(12)
     cases = []

@@ -185,6 +185,54 @@ def test_millions_of_features(dtype, order):
 
 
 @pytest.mark.parametrize("order", [0, 1])
+def test_weights_beyond_32_bit_offsets(order):
+    """More than 2^31 weights, all zero but the first and the last 64 classes: the other
+    classes' logits are 0, and lse, the loss and the gradients follow from 128 classes and
+    the number of the others.  A lane's sum of parts has about a thousand additions."""
+    g = gen(25)
+    kn, ci, t = 16_000_000, 136, 7
+    F = torch.zeros((kn, ci) if order else (ci, kn), dtype=torch.bfloat16, device="cuda")
+    F = F if order else F.t()
+    rows = torch.cat([torch.arange(64, device="cuda"), torch.arange(kn - 64, kn, device="cuda")])
+    F[rows] = (torch.randn(128, ci, generator=g, device="cuda") * 4 * ci ** -0.5).bfloat16()
+    X = stored(g, ci, t, torch.bfloat16)
+    y = torch.tensor([0, 63, kn - 1, kn - 64, 8_000_000, 5, IGNORE], device="cuda")
+    f, x = F[rows].double(), X.double()
+    z = f @ x
+    others = kn - 128
+    lse = torch.log(torch.exp(z).sum(0) + others)
+    zy = torch.stack([z[(rows == c).nonzero()[0, 0], n] if (rows == c).any() else z.new_zeros(()) for n, c in enumerate(y.tolist())])
+    loss = torch.where(y == IGNORE, 0.0, lse - zy)
+    ez = 1.001 * (ci + 6) * truth.EPS * (f.abs() @ x.abs()).max()
+    got, got_lse = lt().linear_cross_entropy(F, X, y)
+    bound = 2 * ez + 1500 * truth.EPS * (1 + lse.abs().max())
+    assert bound < 0.01
+    within(got_lse, lse, bound.expand(t), "lse")
+    within(got, loss, bound.expand(t), "loss")
+    one = torch.full((), 1.0, device="cuda")
+    dX, dF, db = lt().linear_cross_entropy_backward(F, X, y, got_lse, one)
+    d = torch.exp(z - lse)
+    for n, c in enumerate(y.tolist()):
+        d[:, n] -= (rows == c).double()
+    d[:, y == IGNORE] = 0.0
+    u = truth.UNIT[torch.bfloat16]
+    e = u * d.abs() + 4 * bound * torch.exp(z - lse) + 2.0 ** -39
+    want = f.t() @ d
+    within(dX, want, f.abs().t() @ (e * 1.01) + 2 * u * want.abs() + 1e-9, "dX")
+    xk = torch.where(y == IGNORE, 0.0, x)
+    want = d @ xk.t()
+    within(dF[rows], want, (e * 1.01) @ xk.abs().t() + 2 * u * want.abs() + 1e-9, "dF")
+    middle = torch.tensor([64, 7_999_999, 8_000_000, 8_000_001, 1 << 20, kn - 65], device="cuda")
+    p = torch.exp(-lse)[None] - (middle[:, None] == y[None]).double()
+    p[:, y == IGNORE] = 0.0
+    want = p @ xk.t()
+    held = u * p.abs() + 4 * bound * torch.exp(-lse)[None] + 2.0 ** -39
+    within(dF[middle], want, (held * 1.01) @ xk.abs().t() + 2 * u * want.abs() + 1e-9, "dF between")
+    want = d.sum(1)
+    within(db[rows], want, (e * 1.01).sum(1) + 2 * u * want.abs() + 1e-9, "dbias")
+
+
+@pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_several_pieces(dtype, order):
     """More classes than a piece of the gradients holds, the last piece ragged (order 1)
