@@ -190,21 +190,6 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
-// f(chunk, channel of the group) for a group's chunks and channels, dealt out to 256
-// threads.
-template <class F> __device__ inline void each_entry(const Norm& a, F f) {
-  if (a.per >= 256) {
-    for (int k = 0; k < a.chunks; ++k)
-      for (int i = threadIdx.x; i < a.per; i += 256) f(k, i);
-  } else {
-    const int lines = 256 / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
-    if (line < lines) {
-#pragma unroll 4
-      for (int k = line; k < a.chunks; k += lines) f(k, i);
-    }
-  }
-}
-
 // The groups' mean and rstd from their chunks and channels.
 __global__ __launch_bounds__(256) void norm_groups_kernel(Norm a) {
   __shared__ float sh[4];

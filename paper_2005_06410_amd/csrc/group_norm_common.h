@@ -47,6 +47,8 @@ struct Norm {
   Map x, d;                         // input; dO (gradients)
   const void* weight;
   const void* bias;
+  void* dweight;
+  void* dbias;
   int act;
   float eps;
   Map o;                            // O, or dI
@@ -63,7 +65,7 @@ struct Norm {
   // split kernels
   int chunk, chunks;                // positions of a chunk, chunks of an image
   float2* part;                     // [b][chunks][c] mean and squares around it; or [b][groups] averages
-  float* images;                    // gradients: the sums of each image, [b][c] and [b][c], or nullptr
+  int extra;                        // gradients: workgroups that add up dweight and dbias
 };
 
 // How a thread's vector lies: its channels all in one group (per is a multiple of V), so
@@ -372,6 +374,21 @@ __device__ inline float block_sum(float v, float* sh) {
   return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
+// f(chunk, channel of the group) for a group's chunks and channels, dealt out to 256
+// threads.
+template <class F> __device__ inline void each_entry(const Norm& a, F f) {
+  if (a.per >= 256) {
+    for (int k = 0; k < a.chunks; ++k)
+      for (int i = threadIdx.x; i < a.per; i += 256) f(k, i);
+  } else {
+    const int lines = 256 / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
+    if (line < lines) {
+#pragma unroll 4
+      for (int k = line; k < a.chunks; k += lines) f(k, i);
+    }
+  }
+}
+
 template <class T, int MODE> __device__ inline void group_values(const Norm& a, const Place<T, MODE>& p, int64_t* at, float* mean, float* rstd) {
 #pragma unroll
   for (int i = 0; i < kHeld<T, MODE>; ++i) {
@@ -399,7 +416,7 @@ struct NormPlan {
   int threads, held;                 // resident: threads of a workgroup, vectors that a thread holds
   int vecs, units, unit_groups, rows, slots, lanes, shares, blocks;
   int chunk, chunks;
-  int64_t sums, images, stats, bytes;   // byte offsets: part first, then the sums, then mean and rstd
+  int64_t sums, stats, bytes;        // byte offsets: part first, then the sums, then mean and rstd
 };
 
 constexpr int kMostHeld = 8;                       // vectors of a thread
@@ -469,8 +486,7 @@ inline NormPlan plan_of(int dtype, int64_t c, int64_t s, int64_t b, int64_t grou
   p.chunk = (int)(std::min<int64_t>(256, div_up(std::max(div_up(s, want), std::min(s, kAhead * rows)), rows)) * rows);
   p.chunks = (int)div_up(s, p.chunk);
   p.sums = grad ? up(b * groups * 8) : up(b * p.chunks * c * 8);
-  p.images = p.sums + (grad ? up(2 * b * p.chunks * c * 4) : 0);
-  p.stats = p.images + (grad ? up(2 * b * c * 4) : 0);
+  p.stats = p.sums + (grad ? up(2 * b * p.chunks * c * 4) : 0);
   p.bytes = p.stats + (grad ? 0 : 2 * up(b * groups * 4));
   return p;
 }

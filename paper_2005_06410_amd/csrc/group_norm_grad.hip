@@ -210,30 +210,37 @@ template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void no
 }
 
 // dweight and dbias: the parts of a channel added in a fixed order; eight channels of a
-// workgroup, 128 threads each, one output a workgroup.
-template <class T> __global__ __launch_bounds__(1024) void norm_sums_kernel(int c, int64_t parts, const float* __restrict__ sums,
-                                                                            T* __restrict__ dweight, T* __restrict__ dbias) {
-  __shared__ float sh[1024];
-  T* to = blockIdx.y ? dweight : dbias;
+// workgroup, NT / 8 threads each, one output a workgroup (the weights' first).
+template <class T, int NT> __device__ inline void channel_sums(const Norm& a, int block) {
+  __shared__ float sh[NT / 8];
+  const int blocks = (a.c + 7) / 8, which = block >= blocks ? 1 : 0;
+  T* to = static_cast<T*>(which ? a.dbias : a.dweight);
   if (!to) return;
-  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, ch = blockIdx.x * 8 + x;
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, ch = (block - which * blocks) * 8 + x;
   float s = 0.0f;
-  if (ch < c) {
-    const float* p = sums + blockIdx.y * parts * c + ch;
+  if (ch < a.c) {
+    const float* p = a.sums + (which ? 0 : a.parts * a.c) + ch;
+    // 64 at a time, so that a thread's sum stays short
+    for (int64_t lo = y; lo < a.parts; lo += 64 * (NT / 8)) {
+      float t = 0.0f;
 #pragma unroll 8
-    for (int64_t i = y; i < parts; i += 128) s += p[i * c];
+      for (int64_t i = lo; i < min(a.parts, lo + 64 * (NT / 8)); i += NT / 8) t += p[i * a.c];
+      s += t;
+    }
   }
   // lanes eight apart have the same channel
 #pragma unroll
   for (int d = 8; d < 64; d <<= 1) s += __shfl_xor(s, d);
   if ((threadIdx.x & 63) < 8) sh[(threadIdx.x >> 6) * 8 + x] = s;
   __syncthreads();
-  if (y > 0 || ch >= c) return;
+  if (y > 0 || ch >= a.c) return;
   s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += sh[i * 8 + x];
+  for (int i = 0; i < NT / 64; ++i) s += sh[i * 8 + x];
   to[ch] = (T)s;
 }
+
+template <class T, int NT> __global__ __launch_bounds__(NT) void norm_sums_kernel(Norm a) { channel_sums<T, NT>(a, blockIdx.x); }
 
 // Sums of dZ and dZ xhat by chunk and channel.
 template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void norm_slopes_kernel(Norm a) {
@@ -280,60 +287,32 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
-// The sums of a group's channels over its chunks (to a.images), and from them the
-// group's avg d and avg(d xhat).  Narrow groups have 256 / per threads for a channel.
+// The groups' avg d and avg(d xhat) from the sums of their chunks and channels.
 template <class T> __global__ __launch_bounds__(256) void norm_averages_kernel(Norm a) {
-  __shared__ float sh[4], line_s[256], line_x[256];
-  const int lines = a.per < 256 ? 256 / a.per : 1;
-  const int line = a.per < 256 ? threadIdx.x / a.per : 0, i0 = threadIdx.x - line * a.per;
+  __shared__ float sh[4];
+  const T* weight = static_cast<const T*>(a.weight);
+  const float count = (float)a.per * (float)a.s;
   for (int64_t id = blockIdx.x; id < a.b * a.groups; id += gridDim.x) {
-    const int64_t n = id / a.groups, g = id - n * a.groups;
-    const float* from = a.sums + n * a.chunks * a.c + g * a.per;
-    float all_s = 0.0f, all_x = 0.0f;
-    for (int i = i0; i < a.per; i += 256) {
-      float s = 0.0f, sx = 0.0f;
-      if (line < lines) {
-#pragma unroll 4
-        for (int k = line; k < a.chunks; k += lines) {
-          s += from[(int64_t)k * a.c + i];
-          sx += from[(a.parts + k) * a.c + i];
-        }
-      }
-      if (lines > 1) {
-        line_s[threadIdx.x] = s;
-        line_x[threadIdx.x] = sx;
-        __syncthreads();
-        if (line == 0)
-          for (int k = 1; k < lines; ++k) {
-            s += line_s[k * a.per + i];
-            sx += line_x[k * a.per + i];
-          }
-      }
-      if (line == 0) {
-        if (a.images) {
-          a.images[n * a.c + g * a.per + i] = s;
-          a.images[(a.b + n) * a.c + g * a.per + i] = sx;
-        }
-        const float w = a.weight ? (float)static_cast<const T*>(a.weight)[g * a.per + i] : 1.0f;
-        all_s += w * s;
-        all_x += w * sx;
-      }
-    }
-    if (!a.o.p) {
-      __syncthreads();
-      continue;
-    }
-    const float count = (float)a.per * (float)a.s;
-    all_s = block_sum(all_s, sh) / count;
-    all_x = block_sum(all_x, sh) / count;
-    if (threadIdx.x == 0) a.part[id] = float2{all_s, all_x};
-    __syncthreads();
+    const int64_t n = id / a.groups;
+    const int first = (int)(id - n * a.groups) * a.per;
+    const float* from = a.sums + n * a.chunks * a.c + first;
+    float s = 0.0f, sx = 0.0f;
+    each_entry(a, [&](int k, int i) {
+      const float w = weight ? (float)weight[first + i] : 1.0f;
+      s += w * from[(int64_t)k * a.c + i];
+      sx += w * from[(a.parts + k) * a.c + i];
+    });
+    s = block_sum(s, sh) / count;
+    sx = block_sum(sx, sh) / count;
+    if (threadIdx.x == 0) a.part[id] = float2{s, sx};
   }
 }
 
+// The first `extra` workgroups add up dweight and dbias beside the others.
 template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThreads) void norm_dx_kernel(Norm a) {
   constexpr int V = kVec<T>, H = kHeld<T, MODE>;
-  for (int id = blockIdx.x; id < all_parts(a); id += gridDim.x) {
+  if ((int)blockIdx.x < a.extra) return channel_sums<T, kSplitThreads>(a, blockIdx.x);
+  for (int id = blockIdx.x - a.extra; id < all_parts(a); id += gridDim.x - a.extra) {
     const Place<T, MODE> p(a, all_parts(a) - 1 - id);
     if (!p.owner) continue;
     float scale[V], b[V], mean[H], rstd[H], s[H], sx[H];
@@ -362,6 +341,8 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
   }
 }
 
+inline int sums_blocks(const Norm& a) { return 2 * (int)div_up(a.c, 8); }
+
 template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, char* ws, bool want, hipStream_t s) {
   if (p.resident) {
     a.parts = p.blocks;
@@ -382,16 +363,14 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
   }
   a.parts = a.b * p.chunks;
   a.sums = reinterpret_cast<float*>(ws + p.sums);
-  const dim3 grid = grid_of(a.b * p.chunks * p.units);
+  dim3 grid = grid_of(a.b * p.chunks * p.units);
   norm_slopes_kernel<T, MODE><<<grid, kSplitThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  a.images = want ? reinterpret_cast<float*>(ws + p.images) : nullptr;
+  if (e != hipSuccess || !a.o.p) return e;
   norm_averages_kernel<T><<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
-  // dweight and dbias go on from the images' sums
-  a.sums = a.images;
-  a.parts = a.b;
-  if ((e = hipGetLastError()) != hipSuccess || !a.o.p) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  a.extra = want ? sums_blocks(a) : 0;
+  grid.x += a.extra;
   if (streamed<T>(a))
     norm_dx_kernel<T, MODE, true><<<grid, kSplitThreads, 0, s>>>(a);
   else
@@ -411,14 +390,14 @@ template <class T, bool WHOLE> hipError_t launch_feature(const NormPlan& p, cons
   }
 }
 
-template <class T> hipError_t launch_sums(const Norm& a, void* dweight, void* dbias, hipStream_t s) {
-  norm_sums_kernel<T><<<dim3((unsigned)div_up(a.c, 8), 2), 1024, 0, s>>>(a.c, a.parts, a.sums, static_cast<T*>(dweight), static_cast<T*>(dbias));
+template <class T, int NT> hipError_t launch_sums(const Norm& a, hipStream_t s) {
+  norm_sums_kernel<T, NT><<<dim3((unsigned)sums_blocks(a)), NT, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <class T> hipError_t launch_norm_grad(Norm a, const NormPlan& p, char* ws, void* dweight, void* dbias, hipStream_t s) {
+template <class T> hipError_t launch_norm_grad(Norm a, const NormPlan& p, char* ws, hipStream_t s) {
   fill<T>(a, p, ws);
-  const bool want = dweight || dbias;
+  const bool want = a.dweight || a.dbias;
   hipError_t e;
   if (p.feature) {
     a.parts = p.blocks;
@@ -427,7 +406,9 @@ template <class T> hipError_t launch_norm_grad(Norm a, const NormPlan& p, char* 
   } else {
     e = by_mode(p.mode, [&](auto mode) { return launch_mode<T, decltype(mode)::value>(a, p, ws, want, s); });
   }
-  return e != hipSuccess || !want ? e : launch_sums<T>(a, dweight, dbias, s);
+  // split gradients have added them up beside dI already; without it, in the same order
+  if (e != hipSuccess || !want || a.extra) return e;
+  return p.feature || p.resident ? launch_sums<T, 1024>(a, s) : launch_sums<T, kSplitThreads>(a, s);
 }
 
 }  // namespace
@@ -466,16 +447,16 @@ extern "C" int convgemm_group_norm_backward(int dtype, int64_t c, int64_t s, int
   a.x = Map{I, ldi, ldbi};
   a.d = Map{dO, lddo, ldbdo};
   a.o = Map{dI, lddi, ldbdi};
-  a.weight = weight, a.bias = bias, a.act = act;
+  a.weight = weight, a.bias = bias, a.dweight = dweight, a.dbias = dbias, a.act = act;
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
   char* ws = static_cast<char*>(workspace);
   hipError_t e = hipSuccess;
   auto go = [&](auto* none) {
     using T = std::remove_pointer_t<decltype(none)>;
-    if (work) return launch_norm_grad<T>(a, p, ws, dweight, dbias, stream);
+    if (work) return launch_norm_grad<T>(a, p, ws, stream);
     // nothing to add up: zeros
     if (!dweight && !dbias) return hipSuccess;
-    return launch_sums<T>(a, dweight, dbias, stream);
+    return launch_sums<T, kSplitThreads>(a, stream);
   };
   e = dtype == LINEAR_F32 ? go((float*)nullptr) : dtype == LINEAR_BF16 ? go((bf16*)nullptr) : go((f16*)nullptr);
   return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
