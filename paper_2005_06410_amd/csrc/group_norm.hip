@@ -190,21 +190,45 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
+__device__ inline float chunk_length(const Norm& a, int chunk) { return (float)min(a.chunk, a.s - chunk * a.chunk); }
+
+// Mean and squares around it of each channel and image from its chunks, as of one chunk.
+__global__ __launch_bounds__(kJoinThreads) void norm_channels_kernel(Norm a, float2* to) {
+  __shared__ float sh[kJoinThreads];
+  each_channel(a, [&](int64_t n, int ch, bool there, int line) {
+    const float2* from = a.part + n * a.chunks * a.c + ch;
+    float s = 0.0f, q = 0.0f;
+    if (there) {
+#pragma unroll 4
+      for (int k = line; k < a.chunks; k += kChannelLines) s += from[(int64_t)k * a.c].x * chunk_length(a, k);
+    }
+    const float m = channel_sum(s, sh) / (float)a.s;
+    if (there) {
+#pragma unroll 4
+      for (int k = line; k < a.chunks; k += kChannelLines) {
+        const float2 v = from[(int64_t)k * a.c];
+        q += v.y + chunk_length(a, k) * (v.x - m) * (v.x - m);
+      }
+    }
+    q = channel_sum(q, sh);
+    if (there && line == 0) to[n * a.c + ch] = float2{m, q};
+  });
+}
+
 // The groups' mean and rstd from their chunks and channels.
-__global__ __launch_bounds__(256) void norm_groups_kernel(Norm a) {
-  __shared__ float sh[4];
+__global__ __launch_bounds__(kJoinThreads) void norm_groups_kernel(Norm a) {
+  __shared__ float sh[kJoinThreads / 64];
   for (int64_t id = blockIdx.x; id < a.b * a.groups; id += gridDim.x) {
     const int64_t n = id / a.groups;
     const float2* from = a.part + n * a.chunks * a.c + (id - n * a.groups) * a.per;
-    auto length = [&](int chunk) { return (float)min(a.chunk, a.s - chunk * a.chunk); };
     float s = 0.0f;
-    each_entry(a, [&](int k, int i) { s += from[(int64_t)k * a.c + i].x * length(k); });
+    each_entry(a, [&](int k, int i) { s += from[(int64_t)k * a.c + i].x * chunk_length(a, k); });
     const float all = (float)a.per * (float)a.s;
     const float m = block_sum(s, sh) / all;
     s = 0.0f;
     each_entry(a, [&](int k, int i) {
       const float2 v = from[(int64_t)k * a.c + i];
-      s += v.y + length(k) * (v.x - m) * (v.x - m);
+      s += v.y + chunk_length(a, k) * (v.x - m) * (v.x - m);
     });
     s = block_sum(s, sh);
     if (threadIdx.x == 0) {
@@ -260,7 +284,14 @@ template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, c
   norm_stats_kernel<T, MODE><<<grid, kSplitThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  norm_groups_kernel<<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
+  Norm join = a;
+  if (p.wide) {
+    join.part = reinterpret_cast<float2*>(ws + p.joined);
+    join.chunks = 1, join.chunk = a.s;
+    norm_channels_kernel<<<grid_of(a.b * div_up(a.c, 64)), kJoinThreads, 0, s>>>(a, join.part);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  norm_groups_kernel<<<grid_of(a.b * a.groups), kJoinThreads, 0, s>>>(join);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (streamed<T>(a))
     norm_apply_kernel<T, MODE, true><<<grid, kSplitThreads, 0, s>>>(a);

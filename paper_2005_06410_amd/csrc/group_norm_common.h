@@ -365,23 +365,28 @@ template <class T, int MODE> __device__ inline void over_rows(const Norm& a, con
   __syncthreads();
 }
 
-// A sum over 256 threads, in each of them.
+constexpr int kJoinThreads = 1024;
+
+// A sum over all threads of a join, in each of them.
 __device__ inline float block_sum(float v, float* sh) {
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+  v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) v += sh[i];
+  return v;
 }
 
-// f(chunk, channel of the group) for a group's chunks and channels, dealt out to 256
-// threads.
+// f(chunk, channel of the group) for a group's chunks and channels, dealt out to a
+// workgroup's threads.
 template <class F> __device__ inline void each_entry(const Norm& a, F f) {
-  if (a.per >= 256) {
+  if (a.per >= kJoinThreads) {
     for (int k = 0; k < a.chunks; ++k)
-      for (int i = threadIdx.x; i < a.per; i += 256) f(k, i);
+      for (int i = threadIdx.x; i < a.per; i += kJoinThreads) f(k, i);
   } else {
-    const int lines = 256 / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
+    const int lines = kJoinThreads / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
     if (line < lines) {
 #pragma unroll 4
       for (int k = line; k < a.chunks; k += lines) f(k, i);
@@ -395,6 +400,33 @@ template <class T, int MODE> __device__ inline void group_values(const Norm& a, 
     at[i] = p.n * a.groups + min(p.c.ch + i, a.c - 1) / a.per;
     mean[i] = a.mean[at[i]];
     rstd[i] = a.rstd[at[i]];
+  }
+}
+
+// Where a group has many chunks and channels, its chunks are joined channel by channel
+// first: 64 channels of an image in a workgroup, 16 threads for each of them.
+constexpr int kWideEntries = 16384, kChannelLines = kJoinThreads / 64;
+
+// The sum over a channel's threads, in each of them; sh: kJoinThreads floats.
+__device__ inline float channel_sum(float v, float* sh) {
+  const int x = threadIdx.x & 63;
+  __syncthreads();
+  sh[threadIdx.x] = v;
+  __syncthreads();
+  v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kChannelLines; ++i) v += sh[i * 64 + x];
+  return v;
+}
+
+// f(image, channel, whether there is one, this thread's first chunk) for all of them; f
+// is called by whole workgroups.
+template <class F> __device__ inline void each_channel(const Norm& a, F f) {
+  const int blocks = (a.c + 63) / 64;
+  for (int64_t id = blockIdx.x; id < a.b * blocks; id += gridDim.x) {
+    const int64_t n = id / blocks;
+    const int ch = (int)(id - n * blocks) * 64 + (threadIdx.x & 63);
+    f(n, ch, ch < a.c, (int)threadIdx.x >> 6);
   }
 }
 
@@ -412,11 +444,12 @@ inline dim3 grid_of(int64_t parts) { return dim3((unsigned)std::min<int64_t>(par
 
 struct NormPlan {
   bool resident, feature;
+  bool wide;                         // chunks are joined by channel first
   Mode mode;
   int threads, held;                 // resident: threads of a workgroup, vectors that a thread holds
   int vecs, units, unit_groups, rows, slots, lanes, shares, blocks;
   int chunk, chunks;
-  int64_t sums, stats, bytes;        // byte offsets: part first, then the sums, then mean and rstd
+  int64_t sums, joined, stats, bytes;   // byte offsets: part first, then the sums, those by image, mean and rstd
 };
 
 constexpr int kMostHeld = 8;                       // vectors of a thread
@@ -486,7 +519,9 @@ inline NormPlan plan_of(int dtype, int64_t c, int64_t s, int64_t b, int64_t grou
   p.chunk = (int)(std::min<int64_t>(256, div_up(std::max(div_up(s, want), std::min(s, kAhead * rows)), rows)) * rows);
   p.chunks = (int)div_up(s, p.chunk);
   p.sums = grad ? up(b * groups * 8) : up(b * p.chunks * c * 8);
-  p.stats = p.sums + (grad ? up(2 * b * p.chunks * c * 4) : 0);
+  p.wide = p.chunks > 1 && per * p.chunks > kWideEntries;
+  p.joined = p.sums + (grad ? up(2 * b * p.chunks * c * 4) : 0);
+  p.stats = p.joined + (p.wide ? up(b * c * 8) : 0);
   p.bytes = p.stats + (grad ? 0 : 2 * up(b * groups * 4));
   return p;
 }

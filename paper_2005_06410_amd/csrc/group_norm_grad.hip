@@ -287,9 +287,31 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
   }
 }
 
+// The chunks' sums of each channel and image, as of one chunk.
+__global__ __launch_bounds__(kJoinThreads) void norm_chunks_kernel(Norm a, float* to) {
+  __shared__ float sh[kJoinThreads];
+  each_channel(a, [&](int64_t n, int ch, bool there, int line) {
+    const float* from = a.sums + n * a.chunks * a.c + ch;
+    float s = 0.0f, sx = 0.0f;
+    if (there) {
+#pragma unroll 4
+      for (int k = line; k < a.chunks; k += kChannelLines) {
+        s += from[(int64_t)k * a.c];
+        sx += from[(a.parts + k) * a.c];
+      }
+    }
+    s = channel_sum(s, sh);
+    sx = channel_sum(sx, sh);
+    if (there && line == 0) {
+      to[n * a.c + ch] = s;
+      to[(a.b + n) * a.c + ch] = sx;
+    }
+  });
+}
+
 // The groups' avg d and avg(d xhat) from the sums of their chunks and channels.
-template <class T> __global__ __launch_bounds__(256) void norm_averages_kernel(Norm a) {
-  __shared__ float sh[4];
+template <class T> __global__ __launch_bounds__(kJoinThreads) void norm_averages_kernel(Norm a) {
+  __shared__ float sh[kJoinThreads / 64];
   const T* weight = static_cast<const T*>(a.weight);
   const float count = (float)a.per * (float)a.s;
   for (int64_t id = blockIdx.x; id < a.b * a.groups; id += gridDim.x) {
@@ -366,8 +388,17 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
   dim3 grid = grid_of(a.b * p.chunks * p.units);
   norm_slopes_kernel<T, MODE><<<grid, kSplitThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.o.p) return e;
-  norm_averages_kernel<T><<<grid_of(a.b * a.groups), 256, 0, s>>>(a);
+  if (e != hipSuccess) return e;
+  Norm join = a;
+  if (p.wide) {
+    join.sums = reinterpret_cast<float*>(ws + p.joined);
+    join.parts = a.b, join.chunks = 1;
+    norm_chunks_kernel<<<grid_of(a.b * div_up(a.c, 64)), kJoinThreads, 0, s>>>(a, join.sums);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    a.sums = join.sums, a.parts = join.parts;
+  }
+  if (!a.o.p) return e;
+  norm_averages_kernel<T><<<grid_of(a.b * a.groups), kJoinThreads, 0, s>>>(join);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   a.extra = want ? sums_blocks(a) : 0;
   grid.x += a.extra;
