@@ -78,9 +78,10 @@ template <class T, int NT, int RV, int MODE> __global__ __launch_bounds__(NT) vo
   }
 }
 
-template <class T, int RV, int IM, bool WHOLE> __global__ __launch_bounds__(256) void norm_feature_kernel(Norm a) {
+template <class T, int RV, int IM, bool WHOLE, int NT> __global__ __launch_bounds__(NT) void norm_feature_kernel(Norm a) {
   constexpr int V = kVec<T>;
-  const Feature<T, RV, WHOLE> f(a);
+  __shared__ float sh[2][NT / 64];
+  const Feature<T, RV, WHOLE, NT> f(a);
   float w[RV][V], b[RV][V];
 #pragma unroll
   for (int k = 0; k < RV; ++k) {
@@ -103,7 +104,7 @@ template <class T, int RV, int IM, bool WHOLE> __global__ __launch_bounds__(256)
       for (int k = 0; k < RV; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) s += f.any[k] && f.mine(k, i) ? (float)x[m][k].v[i] : 0.0f;
-      mean[m] = f.sum(s, a.lanes) * inverse_n;
+      mean[m] = f.sum(s, a.lanes, sh[0]) * inverse_n;
     }
 #pragma unroll
     for (int m = 0; m < IM; ++m) {
@@ -115,7 +116,7 @@ template <class T, int RV, int IM, bool WHOLE> __global__ __launch_bounds__(256)
           const float d = (float)x[m][k].v[i] - mean[m];
           s += f.any[k] && f.mine(k, i) ? d * d : 0.0f;
         }
-      rstd[m] = 1.0f / sqrtf(f.sum(s, a.lanes) * inverse_n + a.eps);
+      rstd[m] = 1.0f / sqrtf(f.sum(s, a.lanes, sh[1]) * inverse_n + a.eps);
     }
     by_act(a.act, [&](auto act) {
 #pragma unroll
@@ -291,7 +292,7 @@ template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, c
     norm_channels_kernel<<<grid_of(a.b * div_up(a.c, 64)), kJoinThreads, 0, s>>>(a, join.part);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  norm_groups_kernel<<<grid_of(a.b * a.groups), kJoinThreads, 0, s>>>(join);
+  norm_groups_kernel<<<grid_of(a.b * a.groups), join_threads((int64_t)a.per * join.chunks), 0, s>>>(join);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (streamed<T>(a))
     norm_apply_kernel<T, MODE, true><<<grid, kSplitThreads, 0, s>>>(a);
@@ -302,13 +303,20 @@ template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, c
 
 template <class T, bool WHOLE> hipError_t launch_feature(const NormPlan& p, const Norm& a, hipStream_t s) {
   auto go = [&](auto kernel) {
-    kernel<<<dim3((unsigned)((int64_t)p.units * p.blocks)), 256, 0, s>>>(a);
+    kernel<<<dim3((unsigned)((int64_t)p.units * p.blocks)), p.threads, 0, s>>>(a);
     return hipGetLastError();
   };
+  if (p.threads == 512) {
+    switch (p.held) {
+      case 1: return go(norm_feature_kernel<T, 1, 1, WHOLE, 512>);
+      case 2: return go(norm_feature_kernel<T, 2, 1, WHOLE, 512>);
+      default: return go(norm_feature_kernel<T, 4, 1, WHOLE, 512>);
+    }
+  }
   switch (p.held) {
-    case 1: return go(norm_feature_kernel<T, 1, 2, WHOLE>);
-    case 2: return go(norm_feature_kernel<T, 2, 2, WHOLE>);
-    default: return go(norm_feature_kernel<T, 4, 1, WHOLE>);
+    case 1: return go(norm_feature_kernel<T, 1, 2, WHOLE, 256>);
+    case 2: return go(norm_feature_kernel<T, 2, 2, WHOLE, 256>);
+    default: return go(norm_feature_kernel<T, 4, 1, WHOLE, 256>);
   }
 }
 

@@ -65,8 +65,13 @@ struct Norm {
   // split kernels
   int chunk, chunks;                // positions of a chunk, chunks of an image
   float2* part;                     // [b][chunks][c] mean and squares around it; or [b][groups] averages
-  int extra;                        // gradients: workgroups that add up dweight and dbias
+  int extra, span;                  // gradients: workgroups that add up dweight and dbias, channels of one
 };
+
+// Channels from which a workgroup adds up 64 of them, and not 8 (the more threads for
+// each): the gradients of 4096 tokens of 2048 channels fp32 38.2 us, with 8 41.0; of 1024 of 16384
+// bf16 174 and 205.  1000 channels take the same either way.
+constexpr int64_t kSpanChannels = 2048;
 
 // How a thread's vector lies: its channels all in one group (per is a multiple of V), so
 // that what belongs to a group is held once instead of V times; in several groups; in
@@ -225,18 +230,20 @@ template <class T, int NT, int MODE> struct Resident {
 // ---------------------------------------------------------------------------
 // A group of `per` channels lies in `lanes` lanes of one wave, RV vectors each, so that its
 // sums are a few exchanges between lanes, without LDS or barriers; 64 / lanes groups lie side
-// by side.  A wave keeps its groups from image to image.
-template <class T, int RV, bool WHOLE> struct Feature {
-  static constexpr int V = kVec<T>;
+// by side.  A wave keeps its groups from image to image.  Groups too large for a wave (NT =
+// 512) lie in a workgroup, which joins its waves' sums in LDS.  4096 tokens of 8192 channels
+// bf16, one group: 39 us, gradients 93 (split: 277 and 533).
+template <class T, int RV, bool WHOLE, int NT> struct Feature {
+  static constexpr int V = kVec<T>, W = NT == 512 ? 1 : 4;   // images under way in a workgroup
   int64_t n, step;             // this wave's first image and the next one's distance
   int g, at[RV], skip[RV];     // group; first channel of each vector, and channels of it that are the one's before
   bool any[RV];
 
   __device__ Feature(const Norm& a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = 64 / a.lanes;
+    const int lane = threadIdx.x & (NT / W - 1), wave = threadIdx.x / (NT / W), side = NT / W / a.lanes;
     const int sets = a.units, block = blockIdx.x / sets, set = blockIdx.x - block * sets;
-    n = (int64_t)block * 4 + wave;
-    step = (int64_t)a.blocks * 4;
+    n = (int64_t)block * W + wave;
+    step = (int64_t)a.blocks * W;
     g = set * side + lane / a.lanes;
     const int l = lane & (a.lanes - 1);
 #pragma unroll
@@ -268,9 +275,16 @@ template <class T, int RV, bool WHOLE> struct Feature {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = p ? (float)q.v[i] : other;
   }
-  // over the group's lanes
-  __device__ static float sum(float v, int lanes) {
-    for (int d = 1; d < lanes; d <<= 1) v += __shfl_xor(v, d);
+  // over the group's lanes; sh: NT / 64 floats that the sum before did not use
+  __device__ static float sum(float v, int lanes, float* sh) {
+    for (int d = 1; d < min(lanes, 64); d <<= 1) v += __shfl_xor(v, d);
+    if (NT == 512) {
+      if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NT / 64; ++i) v += sh[i];
+    }
     return v;
   }
 };
@@ -365,28 +379,32 @@ template <class T, int MODE> __device__ inline void over_rows(const Norm& a, con
   __syncthreads();
 }
 
+// Joins of a group's chunks have 1024 threads where there is that much to read, or 256 (512 x
+// 100 x 100 fp32, 1 group: 133 us against 773; 60 maps of 31 x 45 x 90, 9 groups: 28.4 against 24.1).
 constexpr int kJoinThreads = 1024;
+inline int join_threads(int64_t entries) { return entries > 2048 ? kJoinThreads : 256; }
 
-// A sum over all threads of a join, in each of them.
+// A sum over all threads of a join, in each of them; sh: kJoinThreads / 64 floats.
 __device__ inline float block_sum(float v, float* sh) {
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 64; ++i) v += sh[i];
+  for (int i = 0; i < (int)blockDim.x / 64; ++i) v += sh[i];
   return v;
 }
 
 // f(chunk, channel of the group) for a group's chunks and channels, dealt out to a
 // workgroup's threads.
 template <class F> __device__ inline void each_entry(const Norm& a, F f) {
-  if (a.per >= kJoinThreads) {
+  const int threads = blockDim.x;
+  if (a.per >= threads) {
     for (int k = 0; k < a.chunks; ++k)
-      for (int i = threadIdx.x; i < a.per; i += kJoinThreads) f(k, i);
+#pragma unroll 4
+      for (int i = threadIdx.x; i < a.per; i += threads) f(k, i);
   } else {
-    const int lines = kJoinThreads / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
+    const int lines = threads / a.per, line = threadIdx.x / a.per, i = threadIdx.x - line * a.per;
     if (line < lines) {
 #pragma unroll 4
       for (int k = line; k < a.chunks; k += lines) f(k, i);
@@ -404,7 +422,10 @@ template <class T, int MODE> __device__ inline void group_values(const Norm& a, 
 }
 
 // Where a group has many chunks and channels, its chunks are joined channel by channel
-// first: 64 channels of an image in a workgroup, 16 threads for each of them.
+// first: 64 channels of an image in a workgroup, 16 threads for each of them.  2 maps of 40 x
+// 40 x 2000 fp16, one group: 36 us (gradients 46) where one workgroup a group took 515 (526).  The
+// limit is where the launch pays: 12800 entries (640 channels of 64 x 64, 32 groups) 23.3 us
+// without it, 28.6 with it; 45000 (300 of 60 x 60, 2 groups) 32.6 and 25.2.
 constexpr int kWideEntries = 16384, kChannelLines = kJoinThreads / 64;
 
 // The sum over a channel's threads, in each of them; sh: kJoinThreads floats.
@@ -446,7 +467,7 @@ struct NormPlan {
   bool resident, feature;
   bool wide;                         // chunks are joined by channel first
   Mode mode;
-  int threads, held;                 // resident: threads of a workgroup, vectors that a thread holds
+  int threads, held;                 // resident and feature: threads of a workgroup, vectors that a thread holds
   int vecs, units, unit_groups, rows, slots, lanes, shares, blocks;
   int chunk, chunks;
   int64_t sums, joined, stats, bytes;   // byte offsets: part first, then the sums, those by image, mean and rstd
@@ -460,15 +481,16 @@ inline NormPlan plan_of(int dtype, int64_t c, int64_t s, int64_t b, int64_t grou
   const int64_t unit = std::min<int64_t>(std::lcm(per, V) / V, all);
   p.mode = per % V == 0 ? kOneGroup : c % V == 0 ? kWhole : c > V ? kTail : kTiny;
   auto fits = [&](int64_t vecs, int threads) { return vecs <= threads && div_up(s, std::max<int64_t>(1, threads / vecs)) <= kMostHeld; };
-  if (s == 1 && per >= V && per <= 64 * V * 4) {
+  if (s == 1 && per >= V && per <= 512 * V * 4) {
     p.feature = true;
-    const int64_t vecs = div_up(per, V);
+    const int64_t vecs = div_up(per, V), lanes = vecs > 64 * 4 ? 512 : 64;
+    p.threads = lanes == 64 ? 256 : 512;
     p.lanes = 1;
-    while (p.lanes < 64 && p.lanes < vecs) p.lanes *= 2;
+    while (p.lanes < lanes && p.lanes < vecs) p.lanes *= 2;
     p.held = 1;
     while (p.held * p.lanes < vecs) p.held *= 2;
-    p.units = (int)div_up(groups, 64 / p.lanes);
-    const int64_t most = std::max<int64_t>(1, 2 * cu / p.units), turns = div_up(b, 4);
+    p.units = (int)div_up(groups, lanes / p.lanes);
+    const int64_t most = std::max<int64_t>(1, 2 * cu / p.units), turns = div_up(b, lanes == 64 ? 4 : 1);
     p.blocks = (int)div_up(turns, div_up(turns, most));
     p.bytes = grad ? up(2 * (int64_t)p.blocks * c * 4) : 0;
     return p;

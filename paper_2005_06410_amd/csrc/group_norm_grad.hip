@@ -126,10 +126,11 @@ template <class T, int NT, int RV, int MODE> __global__ __launch_bounds__(NT) vo
   }
 }
 
-template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void norm_feature_grad_kernel(Norm a) {
+template <class T, int RV, bool WHOLE, int NT> __global__ __launch_bounds__(NT) void norm_feature_grad_kernel(Norm a) {
   constexpr int V = kVec<T>;
-  __shared__ float sh[2][3][64 * RV * V];
-  const Feature<T, RV, WHOLE> f(a);
+  // the sums of three waves, or the two joins of eight
+  __shared__ float sh[2][NT == 512 ? 1 : 3][NT == 512 ? 8 : 64 * RV * V];
+  const Feature<T, RV, WHOLE, NT> f(a);
   float w[RV][V], b[RV][V], total[RV][V], total_x[RV][V];
 #pragma unroll
   for (int k = 0; k < RV; ++k) {
@@ -167,8 +168,8 @@ template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void no
         }
       }
       if (!a.o.p) return;
-      s = f.sum(s, a.lanes) * inverse_n;
-      sx = f.sum(sx, a.lanes) * inverse_n;
+      s = f.sum(s, a.lanes, sh[0][0]) * inverse_n;
+      sx = f.sum(sx, a.lanes, sh[1][0]) * inverse_n;
 #pragma unroll
       for (int k = 0; k < RV; ++k) {
 #pragma unroll
@@ -178,8 +179,8 @@ template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void no
     });
   }
   if (!a.sums) return;
-  // the workgroup's four waves have the same channels
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // four images' waves have the same channels
+  const int lane = threadIdx.x & 63, wave = NT == 512 ? 0 : threadIdx.x >> 6;
   if (wave > 0) {
 #pragma unroll
     for (int k = 0; k < RV; ++k)
@@ -198,7 +199,7 @@ template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void no
     for (int i = 0; i < V; ++i) {
       float s = total[k][i], sx = total_x[k][i];
 #pragma unroll
-      for (int v = 0; v < 3; ++v) {
+      for (int v = 0; v < (NT == 512 ? 0 : 3); ++v) {
         s += sh[0][v][(k * V + i) * 64 + lane];
         sx += sh[1][v][(k * V + i) * 64 + lane];
       }
@@ -209,34 +210,33 @@ template <class T, int RV, bool WHOLE> __global__ __launch_bounds__(256) void no
     }
 }
 
-// dweight and dbias: the parts of a channel added in a fixed order; eight channels of a
-// workgroup, NT / 8 threads each, one output a workgroup (the weights' first).
+// dweight and dbias: the parts of a channel added in a fixed order; a.span (8 or 64)
+// channels of a workgroup, NT / span threads each, one output a workgroup (the weights' first).
 template <class T, int NT> __device__ inline void channel_sums(const Norm& a, int block) {
-  __shared__ float sh[NT / 8];
-  const int blocks = (a.c + 7) / 8, which = block >= blocks ? 1 : 0;
+  __shared__ float sh[NT];
+  const int span = a.span, blocks = (a.c + span - 1) / span, which = block >= blocks ? 1 : 0, lines = NT / span;
   T* to = static_cast<T*>(which ? a.dbias : a.dweight);
   if (!to) return;
-  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, ch = (block - which * blocks) * 8 + x;
+  const int x = threadIdx.x & (span - 1), y = threadIdx.x / span, ch = (block - which * blocks) * span + x;
   float s = 0.0f;
   if (ch < a.c) {
     const float* p = a.sums + (which ? 0 : a.parts * a.c) + ch;
     // 64 at a time, so that a thread's sum stays short
-    for (int64_t lo = y; lo < a.parts; lo += 64 * (NT / 8)) {
+    for (int64_t lo = y; lo < a.parts; lo += 64 * lines) {
       float t = 0.0f;
 #pragma unroll 8
-      for (int64_t i = lo; i < min(a.parts, lo + 64 * (NT / 8)); i += NT / 8) t += p[i * a.c];
+      for (int64_t i = lo; i < min(a.parts, lo + 64 * lines); i += lines) t += p[i * a.c];
       s += t;
     }
   }
-  // lanes eight apart have the same channel
-#pragma unroll
-  for (int d = 8; d < 64; d <<= 1) s += __shfl_xor(s, d);
-  if ((threadIdx.x & 63) < 8) sh[(threadIdx.x >> 6) * 8 + x] = s;
+  // lanes `span` apart have the same channel
+  for (int d = span; d < 64; d <<= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) < span) sh[(threadIdx.x >> 6) * span + x] = s;
   __syncthreads();
   if (y > 0 || ch >= a.c) return;
   s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) s += sh[i * 8 + x];
+  for (int i = 0; i < NT / 64; ++i) s += sh[i * span + x];
   to[ch] = (T)s;
 }
 
@@ -363,7 +363,7 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
   }
 }
 
-inline int sums_blocks(const Norm& a) { return 2 * (int)div_up(a.c, 8); }
+inline int sums_blocks(const Norm& a) { return 2 * (int)div_up(a.c, a.span); }
 
 template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, char* ws, bool want, hipStream_t s) {
   if (p.resident) {
@@ -398,7 +398,7 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
     a.sums = join.sums, a.parts = join.parts;
   }
   if (!a.o.p) return e;
-  norm_averages_kernel<T><<<grid_of(a.b * a.groups), kJoinThreads, 0, s>>>(join);
+  norm_averages_kernel<T><<<grid_of(a.b * a.groups), join_threads((int64_t)a.per * join.chunks), 0, s>>>(join);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   a.extra = want ? sums_blocks(a) : 0;
   grid.x += a.extra;
@@ -411,13 +411,20 @@ template <class T, int MODE> hipError_t launch_mode(Norm& a, const NormPlan& p, 
 
 template <class T, bool WHOLE> hipError_t launch_feature(const NormPlan& p, const Norm& a, hipStream_t s) {
   auto go = [&](auto kernel) {
-    kernel<<<dim3((unsigned)((int64_t)p.units * p.blocks)), 256, 0, s>>>(a);
+    kernel<<<dim3((unsigned)((int64_t)p.units * p.blocks)), p.threads, 0, s>>>(a);
     return hipGetLastError();
   };
+  if (p.threads == 512) {
+    switch (p.held) {
+      case 1: return go(norm_feature_grad_kernel<T, 1, WHOLE, 512>);
+      case 2: return go(norm_feature_grad_kernel<T, 2, WHOLE, 512>);
+      default: return go(norm_feature_grad_kernel<T, 4, WHOLE, 512>);
+    }
+  }
   switch (p.held) {
-    case 1: return go(norm_feature_grad_kernel<T, 1, WHOLE>);
-    case 2: return go(norm_feature_grad_kernel<T, 2, WHOLE>);
-    default: return go(norm_feature_grad_kernel<T, 4, WHOLE>);
+    case 1: return go(norm_feature_grad_kernel<T, 1, WHOLE, 256>);
+    case 2: return go(norm_feature_grad_kernel<T, 2, WHOLE, 256>);
+    default: return go(norm_feature_grad_kernel<T, 4, WHOLE, 256>);
   }
 }
 
@@ -479,6 +486,7 @@ extern "C" int convgemm_group_norm_backward(int dtype, int64_t c, int64_t s, int
   a.d = Map{dO, lddo, ldbdo};
   a.o = Map{dI, lddi, ldbdi};
   a.weight = weight, a.bias = bias, a.dweight = dweight, a.dbias = dbias, a.act = act;
+  a.span = c >= kSpanChannels ? 64 : 8;
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
   char* ws = static_cast<char*>(workspace);
   hipError_t e = hipSuccess;

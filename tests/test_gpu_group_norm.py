@@ -90,6 +90,29 @@ def test_sizes(shape, groups, dtype):
     check(x, dO, groups, w, b, act)
 
 
+# groups of more features than a wave holds, also not whole vectors and of more tokens than
+# workgroups; groups whose chunks are joined by channel first
+WIDE = [((1100, 5), 1), ((2060, 9), 2), ((2052, 3), 1), ((8192, 3), 1), ((4097, 700), 1), ((16384, 2), 1), ((16390, 3), 1), ((9001, 600), 1), ((12300, 1), 2),
+        ((2000, 40, 40, 1), 1), ((515, 70, 70, 2), 1), ((1030, 50, 50, 1), 2), ((6000, 130, 2), 1)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape,groups", WIDE)
+def test_wide_groups(shape, groups, dtype):
+    g = gen(sum(shape))
+    x, dO = maps(g, shape, dtype), maps(g, shape, dtype, offset=0.1)
+    w, b = affine(g, shape[0], dtype)
+    _, mean, rstd, dI, dw, db = check(x, dO, groups, w, b, ACTS[sum(shape) % 5])
+    # what is left out changes nothing in what is not
+    act = ACTS[sum(shape) % 5]
+    for needs in [(1, 0, 0), (0, 1, 1)]:
+        for need, got, v in zip(needs, lt().group_norm_backward(x, dO, groups, mean, rstd, w, b, activation=act, needs=needs), (dI, dw, db)):
+            assert got is None if not need else torch.equal(got, v)
+    # in place
+    want = lt().group_norm(x, groups, w, b, activation=act)[0]
+    assert torch.equal(lt().group_norm(x, groups, w, b, activation=act, out=x)[0], want)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_activations(dtype, act):
