@@ -496,7 +496,7 @@ inline NormPlan plan_of(int dtype, int64_t c, int64_t s, int64_t b, int64_t grou
     return p;
   }
   // resident: 0.2 (0.4) ns a value of one workgroup on a compute unit, and 5 us; split: the
-  // same spread over all units, and what its three (four) launches take
+  // same spread over all units, and what its three launches take
   const double each = (double)unit * V * s * (grad ? 0.4e-3 : 0.2e-3), rounds = (double)div_up(div_up(all, unit) * b, cu);
   const double split = (grad ? 28.0 : 18.0) + each * div_up(all, unit) * b / cu;
   if (fits(unit, p.mode == kTiny ? 256 : 512) && 5.0 + each * rounds <= split) {
