@@ -13,7 +13,7 @@ template <class T, int NT, int RV, int MODE> __global__ __launch_bounds__(NT) vo
   float w[V], b[V];
   c.values(a.weight, 1.0f, w);
   c.values(a.bias, 0.0f, b);
-  const float inverse_n = 1.0f / ((float)a.per * (float)a.s);
+  const Count count((float)a.per * (float)a.s);
   for (int64_t n0 = (int64_t)r.block * a.slots; n0 < a.b; n0 += (int64_t)a.blocks * a.slots) {
     const int64_t n = n0 + r.slot;
     const bool there = r.owner && n < a.b;
@@ -35,7 +35,7 @@ template <class T, int NT, int RV, int MODE> __global__ __launch_bounds__(NT) vo
       }
     r.group_sums(c, mean);
 #pragma unroll
-    for (int i = 0; i < H; ++i) mean[0][i] *= inverse_n;
+    for (int i = 0; i < H; ++i) mean[0][i] = count.quotient(mean[0][i]);
 #pragma unroll
     for (int k = 0; k < RV; ++k)
       if (there && r.row + k * a.rows < a.s) {
@@ -47,7 +47,7 @@ template <class T, int NT, int RV, int MODE> __global__ __launch_bounds__(NT) vo
       }
     r.group_sums(c, rstd);
 #pragma unroll
-    for (int i = 0; i < H; ++i) rstd[0][i] = 1.0f / sqrtf(rstd[0][i] * inverse_n + a.eps);
+    for (int i = 0; i < H; ++i) rstd[0][i] = rstd_of(rstd[0][i], count, a.eps);
     if (there && r.row == 0) {
       // the threads that have a group's first channel
 #pragma unroll
@@ -88,7 +88,7 @@ template <class T, int RV, int IM, bool WHOLE, int NT> __global__ __launch_bound
     f.values(a.weight, 1.0f, k, w[k]);
     f.values(a.bias, 0.0f, k, b[k]);
   }
-  const float inverse_n = 1.0f / (float)a.per;
+  const Count count((float)a.per);
   for (int64_t n0 = f.n; n0 < a.b; n0 += IM * f.step) {
     Packed<T> x[IM][RV];
     float mean[IM], rstd[IM];
@@ -104,7 +104,7 @@ template <class T, int RV, int IM, bool WHOLE, int NT> __global__ __launch_bound
       for (int k = 0; k < RV; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) s += f.any[k] && f.mine(k, i) ? (float)x[m][k].v[i] : 0.0f;
-      mean[m] = f.sum(s, a.lanes, sh[0]) * inverse_n;
+      mean[m] = count.quotient(f.sum(s, a.lanes, sh[0]));
     }
 #pragma unroll
     for (int m = 0; m < IM; ++m) {
@@ -116,7 +116,7 @@ template <class T, int RV, int IM, bool WHOLE, int NT> __global__ __launch_bound
           const float d = (float)x[m][k].v[i] - mean[m];
           s += f.any[k] && f.mine(k, i) ? d * d : 0.0f;
         }
-      rstd[m] = 1.0f / sqrtf(f.sum(s, a.lanes, sh[1]) * inverse_n + a.eps);
+      rstd[m] = rstd_of(f.sum(s, a.lanes, sh[1]), count, a.eps);
     }
     by_act(a.act, [&](auto act) {
 #pragma unroll
@@ -174,10 +174,10 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
       s[i] = first[i] * count;
     }
     over_rows<T, MODE>(a, p, sh, s, mean);
-    const float n = 1.0f / (float)(p.hi - p.lo);
+    const Count n((float)(p.hi - p.lo));
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      mean[i] *= n;
+      mean[i] = n.quotient(mean[i]);
       const float d = first[i] - mean[i];
       q[i] += mine ? count * d * d : 0.0f;
     }
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kJoinThreads) void norm_groups_kernel(Norm a) {
     s = block_sum(s, sh);
     if (threadIdx.x == 0) {
       a.mean[id] = m;
-      a.rstd[id] = 1.0f / sqrtf(s / all + a.eps);
+      a.rstd[id] = rstd_of(s, Count(all), a.eps);
     }
   }
 }

@@ -132,6 +132,33 @@ template <class F> __device__ inline void by_act(int act, F f) {
   with_act(act, f);
 }
 
+// sum / n rounded once, by n's inverse and what the product loses: three operations
+// where a division takes ten (27 x 27 x 256 x 80 fp32, 32 groups: 25.9 us, with divisions and a
+// root 28.8).  The inverse's rounding alone would be the same way in every group.
+struct Count {
+  float n, inverse;
+  __device__ explicit Count(float v) : n(v), inverse(1.0f / v) {}
+  __device__ float quotient(float sum, float* lost = nullptr) const {
+    const float first = sum * inverse, q = fmaf(fmaf(-first, n, sum), inverse, first);
+    if (lost) *lost = fmaf(-q, n, sum) * inverse;
+    return q;
+  }
+};
+
+// 1 / sqrt(sum / n + eps), rounded about once, since what follows multiplies by it: the
+// quotient and the sum with what their roundings lose, the hardware's root and one step of
+// Newton's.
+__device__ inline float rstd_of(float sum, const Count& n, float eps) {
+  float lost;
+  const float q = n.quotient(sum, &lost), v = q + eps, e = v - q;
+  lost += (q - (v - e)) + (eps - e);
+  // no sum of normal size (0 and NaN among them) has a finite root to go on from
+  if (!(v >= 1.17549435e-38f && v < INFINITY)) return 1.0f / sqrtf(v);
+  const float r = __builtin_amdgcn_rsqf(v), p = v * r;
+  const float left = fmaf(-p, r, 1.0f) - (fmaf(v, r, -p) + lost * r) * r;   // 1 - (v + lost) r^2
+  return fmaf(0.5f * r, left, r);
+}
+
 // ---------------------------------------------------------------------------
 // resident: a unit (whole groups, whole vectors) of an image in registers
 // ---------------------------------------------------------------------------

@@ -1,0 +1,69 @@
+"""Group norm's mean and rstd: rounded about once, also where a rounding of theirs decides
+on which side of relu's border a value lies."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+# (c, s, b), groups: in a workgroup's registers (one group a vector, several, vectors that are not
+# whole, a few channels), and the features of tokens in a wave and in a workgroup
+ONE_READ = [((6, 5, 3), 2), ((3, 35, 2), 3), ((90, 45, 7), 9), ((256, 729, 2), 32), ((64, 169, 3), 32), ((40, 16, 65), 4), ((1000, 1, 41), 8),
+            ((4001, 1, 5), 1), ((8192, 1, 3), 1)]
+
+
+def lt():
+    import paper_2005_06410_amd as m
+    return m
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def stored(v, dtype):
+    """(c, s, b) values with the channels fastest."""
+    return v.permute(2, 1, 0).contiguous().to(dtype).permute(2, 1, 0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape,groups", ONE_READ)
+def test_mean_is_rounded_once(shape, groups, dtype):
+    """Whole numbers below 16: their sums are exact in fp32 (n 15 < 2^24), and the mean is the
+    quotient's one rounding."""
+    c, s, b = shape
+    x = stored(torch.randint(0, 16, shape, generator=gen(c + s), device="cuda"), dtype)
+    _, mean, _ = lt().group_norm(x, groups)
+    n = c // groups * s
+    want = x.double().reshape(groups, n, b).sum(1) / n
+    assert torch.equal(mean, want.float())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape,groups", ONE_READ)
+def test_rstd_is_rounded_once(shape, groups, dtype):
+    """Whole numbers that lie evenly around 3: mean, differences and squares are exact, and so
+    is eps.  The quotient, the sum and the step keep what their roundings lose but for second
+    orders (2^-44 in all), the last sum is rounded once: 2^-24 (1 + 2^-16) of rstd."""
+    c, s, b = shape
+    n = c // groups * s
+    half = torch.randint(-7, 8, (groups, n // 2, b), generator=gen(c + s), device="cuda")
+    e = torch.cat([half, torch.zeros((groups, n % 2, b), device="cuda", dtype=half.dtype), -half], 1)
+    x = stored(3 + e.reshape(shape), dtype)
+    eps = 2.0 ** -10
+    _, mean, rstd = lt().group_norm(x, groups, eps=eps)
+    assert (mean == 3).all()
+    want = ((e.double() ** 2).sum(1) / n + eps) ** -0.5
+    off = (rstd.double() / want - 1).abs()
+    assert (off <= 2.0 ** -24 * (1 + 2.0 ** -16)).all(), float(off.max()) * 2.0 ** 24
+
+
+def test_rstd_without_variance():
+    """Where the variance is 0, rstd is 1 / sqrt(eps), and infinite where eps is 0 too."""
+    x = stored(torch.full((8, 9, 2), 3.0, device="cuda"), torch.float32)
+    for eps in (0.0, 2.0 ** -10, 2.0 ** -100):
+        _, mean, rstd = lt().group_norm(x, 2, eps=eps)
+        want = torch.tensor(eps, dtype=torch.float64, device="cuda") ** -0.5
+        assert (mean == 3).all() and (rstd.double() == want).all()
