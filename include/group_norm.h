@@ -16,8 +16,8 @@
  *
  * Types: I, O, weight, bias and the gradients are LINEAR_F32, LINEAR_BF16 or LINEAR_F16;
  * mean and rstd are fp32.  Everything is computed in fp32: the mean first and the squares
- * around it (or around a value of the part, parts then joined by their means), never as
- * a difference of two large sums; each result is rounded once.  A group that holds
+ * around it (or four values at a time around the mean of those before, parts then joined by
+ * their means), never as a difference of two large sums; each result is rounded once.  A group that holds
  * an infinity or a NaN gives NaN, and only that group.  Every result is reproducible.
  *
  * Storage: channels are neighbours; position p of image n starts at p ld + n ldb values,

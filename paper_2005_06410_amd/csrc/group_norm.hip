@@ -139,38 +139,57 @@ template <class T, int RV, int IM, bool WHOLE, int NT> __global__ __launch_bound
   }
 }
 
-// Mean and squares around it of each channel over a chunk: a thread sums differences
-// to its first value, then the threads are joined by their means.
+// Mean and squares around it of each channel over a chunk: a thread takes its values
+// relative to its first one, four at a time around the mean of those before,
+//   d = x - mean,   mean += sum d / n,   squares += sum d^2 - (sum d)^2 / n,
+// n with the four.  At least half of sum d^2 stays (a quarter of the first four), whatever lies
+// far from the others; relative to the first value alone, a far one there left the difference of
+// sums as large as all of them (a value of 10^6 before 256 of 0.1: rstd off by 3e-4).  Then the
+// threads are joined by their means.
 template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void norm_stats_kernel(Norm a) {
   constexpr int V = kVec<T>;
   __shared__ float sh[(kSplitThreads + 256) * V];
   for (int id = blockIdx.x; id < all_parts(a); id += gridDim.x) {
     const Place<T, MODE> p(a, id);
-    float first[V], s[V], q[V];
+    float first[V], m[V], s[V], q[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) first[i] = s[i] = q[i] = 0.0f;
-    const int mine = p.owner && p.lo + p.row < p.hi ? (p.hi - p.lo - p.row + p.rows - 1) / p.rows : 0;
-    if (mine)
-      each_position<T, MODE, false>(
-          a, p,
-          [&](const Packed<T>& x) {
+    for (int i = 0; i < V; ++i) first[i] = m[i] = q[i] = 0.0f;
+    int mine = 0;
+    if (p.owner)
+      each_batch<T, MODE, false>(a, p, [&](int at, const Packed<T>(&x)[kAhead], const Packed<T>(&)[kAhead]) {
+        if (mine == 0) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) first[i] = (float)x.v[i];
-          },
-          [&](int, const Packed<T>& x, const Packed<T>&) {
+          for (int i = 0; i < V; ++i) first[i] = (float)x[0].v[i];
+        }
+        // COUNT values from the k-th on
+        auto take = [&](int k, auto COUNT) {
+          constexpr int count = decltype(COUNT)::value;
+          mine += count;
+          const float over = __builtin_amdgcn_rcpf((float)mine);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const float d = (float)x.v[i] - first[i];
-              s[i] += d;
-              q[i] += d * d;
+          for (int i = 0; i < V; ++i) {
+            float sum = 0.0f, squares = 0.0f;
+#pragma unroll
+            for (int j = 0; j < count; ++j) {
+              const float d = (float)x[k + j].v[i] - first[i] - m[i];
+              sum += d;
+              squares += d * d;
             }
-          });
-    const float count = (float)mine, over = mine ? 1.0f / count : 0.0f;
+            const float by = sum * over;
+            m[i] += by;
+            q[i] += squares - by * sum;
+          }
+        };
+        if (at + (kAhead - 1) * p.rows < p.hi) return take(0, std::integral_constant<int, kAhead>{});
+#pragma unroll
+        for (int k = 0; k < kAhead - 1; ++k)
+          if (at + k * p.rows < p.hi) take(k, std::integral_constant<int, 1>{});
+      });
+    const float count = (float)mine;
     float mean[V], square[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      q[i] -= s[i] * s[i] * over;
-      first[i] += s[i] * over;              // this thread's mean
+      first[i] += m[i];                     // this thread's mean
       s[i] = first[i] * count;
     }
     over_rows<T, MODE>(a, p, sh, s, mean);
@@ -255,7 +274,7 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
     for (int i = 0; i < V; ++i) scale[i] *= rstd[MODE == kOneGroup ? 0 : i];
     T* to = static_cast<T*>(const_cast<void*>(a.o.p)) + p.n * a.o.ldb + p.c.ch;
     by_act(a.act, [&](auto act) {
-      each_position<T, MODE, false>(a, p, [](const Packed<T>&) {}, [&](int q, const Packed<T>& x, const Packed<T>&) {
+      each_position<T, MODE, false>(a, p, [&](int q, const Packed<T>& x, const Packed<T>&) {
         float z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] = act_value<T, decltype(act)::value>(((float)x.v[i] - mean[MODE == kOneGroup ? 0 : i]) * scale[i] + b[i]);

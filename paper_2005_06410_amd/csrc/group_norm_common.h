@@ -351,14 +351,12 @@ template <class T, int MODE> struct Place {
 // Below 2^31: a part has thousands of values, and all of them are below 2^40.
 __device__ inline int all_parts(const Norm& a) { return (int)a.b * a.chunks * a.units; }
 
-// f(position, vectors) for every position of this thread; kAhead loads of each input
-// are issued before the first is used, since what f stores may be the input itself.
-// start(vector) gets the first one.
-template <class T, int MODE, bool TWO, class S, class F>
-__device__ inline void each_position(const Norm& a, const Place<T, MODE>& p, S start, F f) {
+// f(first position, vectors) for the positions of this thread, up to kAhead at a
+// time, `rows` apart; all loads are issued before the first is used, since what f stores may
+// be the input itself.
+template <class T, int MODE, bool TWO, class F> __device__ inline void each_batch(const Norm& a, const Place<T, MODE>& p, F f) {
   const T* x = static_cast<const T*>(a.x.p) + p.n * a.x.ldb + p.c.ch;
   const T* d = TWO ? static_cast<const T*>(a.d.p) + p.n * a.d.ldb + p.c.ch : x;
-  bool first = true;
   for (int at = p.lo + p.row; at < p.hi; at += kAhead * p.rows) {
     Packed<T> vx[kAhead], vd[kAhead];
 #pragma unroll
@@ -368,14 +366,19 @@ __device__ inline void each_position(const Norm& a, const Place<T, MODE>& p, S s
       vx[k] = p.c.read(x + q * a.x.ld);
       if (TWO) vd[k] = p.c.read(d + q * a.d.ld);
     }
-    if (first) start(vx[0]);
-    first = false;
+    f(at, vx, vd);
+  }
+}
+
+// f(position, vectors) for every position of this thread.
+template <class T, int MODE, bool TWO, class F> __device__ inline void each_position(const Norm& a, const Place<T, MODE>& p, F f) {
+  each_batch<T, MODE, TWO>(a, p, [&](int at, const Packed<T>(&vx)[kAhead], const Packed<T>(&vd)[kAhead]) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int q = at + k * p.rows;
       if (q < p.hi) f(q, vx[k], vd[k]);
     }
-  }
+  });
 }
 
 // The sums over the workgroup's rows of one value by channel and thread, in every

@@ -260,7 +260,7 @@ template <class T, int MODE> __global__ __launch_bounds__(kSplitThreads) void no
 #pragma unroll
       for (int i = 0; i < V; ++i) scale[i] *= rstd[MODE == kOneGroup ? 0 : i];
       by_act(a.act, [&](auto act) {
-        each_position<T, MODE, true>(a, p, [](const Packed<T>&) {}, [&](int, const Packed<T>& x, const Packed<T>& d) {
+        each_position<T, MODE, true>(a, p, [&](int, const Packed<T>& x, const Packed<T>& d) {
           float dz[V], t[V];
           slopes<T, decltype(act)::value, MODE>(x, d, mean, scale, b, dz, t);
 #pragma unroll
@@ -352,7 +352,7 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
     for (int i = 0; i < V; ++i) scale[i] *= rstd[MODE == kOneGroup ? 0 : i];
     T* to = static_cast<T*>(const_cast<void*>(a.o.p)) + p.n * a.o.ldb + p.c.ch;
     by_act(a.act, [&](auto act) {
-      each_position<T, MODE, true>(a, p, [](const Packed<T>&) {}, [&](int q, const Packed<T>& x, const Packed<T>& d) {
+      each_position<T, MODE, true>(a, p, [&](int q, const Packed<T>& x, const Packed<T>& d) {
         float dz[V], t[V];
         slopes<T, decltype(act)::value, MODE>(x, d, mean, scale, b, dz, t);
 #pragma unroll

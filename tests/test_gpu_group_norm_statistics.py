@@ -67,3 +67,43 @@ def test_rstd_without_variance():
         _, mean, rstd = lt().group_norm(x, 2, eps=eps)
         want = torch.tensor(eps, dtype=torch.float64, device="cuda") ** -0.5
         assert (mean == 3).all() and (rstd.double() == want).all()
+
+
+# (c, s, b), groups, and the values of a channel that a thread takes at the most
+CHUNKED = [((32, 25600, 1), 8, 4), ((16, 1 << 19, 2), 4, 16), ((16, (1 << 24) - 1, 1), 4, 64), ((4, 65536, 4100), 1, 256)]
+
+
+@pytest.mark.parametrize("far", [200.0, 12345.678, 1e6])
+@pytest.mark.parametrize("base", [None, 0.1])
+@pytest.mark.parametrize("shape,groups,held", CHUNKED)
+def test_a_far_first_value(shape, groups, held, base, far):
+    """Large maps in chunks whose first position holds a value far from all others, which are
+    normal or all the same: most of the variance is that value's, and what the thread that met
+    it first makes of it shows whole.
+
+    In units of 2^-24 of the sum of squares: four values' squares and their sum's square are off by
+    20 of the squares, of which a quarter or more stays: 80; what a thread adds up, one each
+    of held / 4 steps; its mean is off by two of the far value a step, which enters the
+    squares around the chunk's mean twice: together 5 a step, 5 / 4 held; the others' differences, which are
+    rounded at the far value's size, at most 16; the sums over threads, chunks and channels
+    pass at most 64 additions.  rstd is off by half of all this and its own rounding.  The
+    mean: 64 additions of the values' size, and in the threads that begin with the far value
+    two roundings of it a step."""
+    c, s, b = shape
+    n = c // groups * s
+    x = torch.empty((b, s, c), device="cuda")
+    if base is None:
+        x.normal_(generator=gen(c))
+    else:
+        x.fill_(base)
+    x[:, 0] = far
+    _, mean, rstd = lt().group_norm(x.permute(2, 1, 0), groups, eps=2.0 ** -20)
+    for image in {0, b - 1}:
+        v = x[image].double().reshape(s, groups, c // groups)
+        m = v.mean((0, 2))
+        want = ((v - m[:, None]) ** 2).mean((0, 2)).add(2.0 ** -20) ** -0.5
+        off = (rstd[:, image].double() / want - 1).abs()
+        bound = (160 + 5 * held / 4) / 2 * 2.0 ** -24 + 2.0 ** -24
+        assert (off <= bound).all(), f"rstd is off by {float(off.max()):.3g}, {float(off.max()) / bound:.3g} times its bound"
+        size = v.abs().mean((0, 2))
+        assert ((mean[:, image].double() - m).abs() <= 2.0 ** -24 * (64 * size + far * held * held / 2 / s)).all()
