@@ -49,7 +49,7 @@ int64_t convgemm_group_norm_backward_workspace(int dtype, int64_t c, int64_t s, 
  *   groups            : >= 1, divides c;
  *   weight, bias      : c values each, or NULL (1 and 0);
  *   eps               : >= 0;
- *   mean, rstd        : groups x b values, groups fastest, or NULL. */
+ *   mean, rstd        : groups x b values, groups fastest, or NULL; NaN where c s = 0. */
 int convgemm_group_norm(int dtype, int64_t c, int64_t s, int64_t b, int64_t groups, const void* I, int64_t ldi, int64_t ldbi,
                         const void* weight, const void* bias, double eps, int act, void* O, int64_t ldo, int64_t ldbo,
                         float* mean, float* rstd, void* workspace, int64_t workspace_bytes, hipStream_t stream);

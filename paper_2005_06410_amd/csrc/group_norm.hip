@@ -284,6 +284,14 @@ template <class T, int MODE, bool STREAM> __global__ __launch_bounds__(kSplitThr
   }
 }
 
+// The mean and rstd of no values: 0 / 0.
+__global__ __launch_bounds__(256) void norm_nothing_kernel(int64_t count, float* mean, float* rstd) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+    if (mean) mean[i] = NAN;
+    if (rstd) rstd[i] = NAN;
+  }
+}
+
 template <class T, int MODE> hipError_t launch_mode(Norm a, const NormPlan& p, char* ws, hipStream_t s) {
   if (p.resident) {
     const int64_t floats = p.threads * (int64_t)kHeld<T, MODE> + (int64_t)p.slots * p.unit_groups * p.shares;
@@ -366,7 +374,12 @@ extern "C" int convgemm_group_norm(int dtype, int64_t c, int64_t s, int64_t b, i
   if (act < LINEAR_ACT_NONE || act > LINEAR_ACT_SILU) return -12;
   if (!O && work) return -13;
   if (int e = check_map(c, s, b, ldo, ldbo, 14)) return e;
-  if (!work) return LINEAR_OK;
+  if (!work) {
+    if (b == 0 || (!mean && !rstd)) return LINEAR_OK;
+    norm_nothing_kernel<<<grid_of(div_up(groups * b, 256)), 256, 0, stream>>>(groups * b, mean, rstd);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LINEAR_OK : LINEAR_ERR_HIP_BASE - (int)e;
+  }
   const NormPlan p = plan_of(dtype, c, s, b, groups, false);
   if (p.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return -18;
   if (workspace_bytes < p.bytes) return -19;

@@ -107,3 +107,22 @@ def test_a_far_first_value(shape, groups, held, base, far):
         assert (off <= bound).all(), f"rstd is off by {float(off.max()):.3g}, {float(off.max()) / bound:.3g} times its bound"
         size = v.abs().mean((0, 2))
         assert ((mean[:, image].double() - m).abs() <= 2.0 ** -24 * (64 * size + far * held * held / 2 / s)).all()
+
+
+@pytest.mark.parametrize("shape,groups", [((0, 4, 3), 1), ((8, 0, 5), 4), ((8, 0, 300000), 2), ((8, 4, 0), 2)])
+def test_statistics_of_nothing(shape, groups):
+    """Images without a value have the mean 0 / 0; without images there is nothing to write."""
+    c, s, b = shape
+    size = (1, c, s, b, groups)
+    apart = (max(c, 1), max(c, 1) * max(s, 1))
+    stream = torch.cuda.current_stream().cuda_stream
+    for which in ((0, 1), (0,), (1,), ()):
+        held = torch.full((2, groups * b + 8), 5.0, device="cuda")
+        at = [held[i].data_ptr() if i in which else 0 for i in range(2)]
+        assert lt().load().convgemm_group_norm(*size, 0, *apart, 0, 0, 1e-5, 0, 0, *apart, *at, 0, 0, stream) == 0
+        for i in range(2):
+            written = groups * b if i in which else 0
+            assert held[i, :written].isnan().all() and (held[i, written:] == 5).all()
+    x = torch.empty((b, s, c), device="cuda").permute(2, 1, 0)
+    _, mean, rstd = lt().group_norm(x, groups)
+    assert mean.shape == rstd.shape == (groups, b) and mean.isnan().all() and rstd.isnan().all()
