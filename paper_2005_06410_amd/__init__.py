@@ -968,6 +968,32 @@ def _span(v, b: int, s: int, c: int, ld: int, ldb: int):
     return at, at + ((b - 1) * ldb + (s - 1) * ld + c) * v.element_size()
 
 
+def _maps_meet(c: int, s: int, b: int, x: int, ldx: int, ldbx: int, o: int, ldo: int, ldbo: int) -> bool:
+    """Whether two maps of c s b values (at the addresses x and o, in values) share one.
+    Maps at different distances of which both have gaps are taken to where their spans
+    meet."""
+    if c * s * b == 0:
+        return False
+    if o + (b - 1) * ldbo + (s - 1) * ldo + c <= x or x + (b - 1) * ldbx + (s - 1) * ldx + c <= o:
+        return False
+    if b == 1:                                       # the images' distance does not matter
+        ldbx, ldbo = s * ldx, s * ldo
+    if s == 1:                                       # nor does the positions'
+        ldx, ldo = ldbx, ldbo
+    if (ldx, ldbx) == (ldo, ldbo):
+        # o - x = i ldb + p ld + k for some |i| < b, |p| < s, |k| < c: the last two together lie
+        # within ldb and the last within ld, so that two i and two p can be meant
+        for i in ((o - x) // ldbx, (o - x) // ldbx + 1):
+            rest = o - x - i * ldbx
+            for p in (rest // ldx, rest // ldx + 1):
+                if abs(i) < b and abs(p) < s and abs(rest - p * ldx) < c:
+                    return True
+        return False
+    if ldbx == s * ldx and ldbo == s * ldo and (ldx == c or ldo == c):
+        return _meet(x, c, s * b, ldx, o, c, s * b, ldo)
+    return True
+
+
 def group_norm(I, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", out=None):
     """O = act(weight (I - mean) rstd + bias), mean and variance over each of ``groups``
     runs of channels and all positions of an image (``convgemm_group_norm``).
@@ -992,8 +1018,8 @@ def group_norm(I, groups: int, weight=None, bias=None, eps: float = 1e-5, activa
         if c * s * b:
             span, size = _span(out, b, s, c, *disto), I.element_size()
             itself = out.data_ptr() == I.data_ptr() and disto[0] == dist[0] and (disto[1] == dist[1] or b == 1)
-            inputs = [(p, p + c * size) for p in (wp, bp) if p] + ([] if itself else [_span(I, b, s, c, *dist)])
-            if any(lo < span[1] and span[0] < hi for lo, hi in inputs):
+            if (any(p < span[1] and span[0] < p + c * size for p in (wp, bp) if p)
+                    or (not itself and _maps_meet(c, s, b, I.data_ptr() // size, *dist, out.data_ptr() // size, *disto))):
                 raise ValueError("out may not overlap an input other than I itself")
     f32 = _torch().float32
     mean, rstd = I.new_empty_strided((groups, b), (1, groups), dtype=f32), I.new_empty_strided((groups, b), (1, groups), dtype=f32)
