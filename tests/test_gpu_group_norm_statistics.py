@@ -126,3 +126,21 @@ def test_statistics_of_nothing(shape, groups):
     x = torch.empty((b, s, c), device="cuda").permute(2, 1, 0)
     _, mean, rstd = lt().group_norm(x, groups)
     assert mean.shape == rstd.shape == (groups, b) and mean.isnan().all() and rstd.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape,groups", ONE_READ + [((30, 22650, 2), 5), ((7, 20011, 2), 7), ((12, 40000, 1), 1)])
+def test_gradients_of_scaled_inputs(shape, groups, dtype):
+    """Inputs of 2^-k times the size, and rstd 2^k times as large: dI is 2^k times as large and
+    the others are the same, bit for bit, since nothing is rounded differently."""
+    c, s, b = shape
+    g = gen(c + s)
+    x, dO = (stored(torch.randn(shape, generator=g, device="cuda"), dtype) for _ in range(2))
+    w, bias = ((at + 0.3 * torch.randn(c, generator=g, device="cuda")).to(dtype) for at in (1, 0))
+    _, mean, rstd = lt().group_norm(x, groups, w, bias)
+    want = lt().group_norm_backward(x, dO, groups, mean, rstd, w, bias, activation="silu")
+    for k in (-60, 50, 66, 90):
+        got = lt().group_norm_backward(x * 2.0 ** -k, dO, groups, mean * 2.0 ** -k, rstd * 2.0 ** k, w, bias, activation="silu")
+        # what is near bf16's or fp32's smallest values is rounded there
+        assert torch.equal(torch.where(want[0].abs() < 2.0 ** -60, 0, got[0]), torch.where(want[0].abs() < 2.0 ** -60, 0, want[0]) * 2.0 ** k)
+        assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
