@@ -17,7 +17,10 @@
  * Types: I, O, weight, bias and the gradients are LINEAR_F32, LINEAR_BF16 or LINEAR_F16;
  * mean and rstd are fp32.  Everything is computed in fp32: the mean first and the squares
  * around it (or four values at a time around the mean of those before, parts then joined by
- * their means), never as a difference of two large sums; each result is rounded once.  A group that holds
+ * their means), never as a difference of two large sums; each result is rounded once.
+ * relu's slope jumps where Z = 0: it goes by Z as computed from the fp32 mean and rstd, and
+ * a Z within their roundings of 0 may fall on the other side than in exact arithmetic; a
+ * whole dO is then in or out of the gradients.  A group that holds
  * an infinity or a NaN gives NaN, and only that group.  Every result is reproducible.
  *
  * Storage: channels are neighbours; position p of image n starts at p ld + n ldb values,

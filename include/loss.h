@@ -23,15 +23,18 @@
  *
  * g_n = dL/dloss_n; gradients: dX = F^T dZ, dF = dZ X^T, dbias = dZ 1.  A column with
  * g_n = 0, or one that does not count, adds nothing to dF and dbias even where X or Z
- * are infinite or NaN there or its target is invalid, and its dX is zero.
+ * are infinite or NaN there or its target is invalid; its dX is zero where F is finite
+ * (a product with zeros, so that an infinity or a NaN of F makes it NaN).
  *
  * Classes can be masked by a bias of -infinity: p is 0 there.  A column in which every
  * class is masked has lse = -infinity and NaN gradients.
  *
  * Types: F, X, bias, dX, dF and dbias are LINEAR_F32, LINEAR_BF16 or LINEAR_F16
  * (linear.h); losses, lse and g are fp32.  Z is summed in fp32, and everything up to
- * the loss is computed in fp32.  The gradients compute Z again, a piece of the classes
- * at a time (8192 or more); a piece's dZ is held in the layer's type, one rounding
+ * the loss is computed in fp32; exponentials of 16-bit layers' Z are the hardware's, off by
+ * up to about 2^-22, also in the fp32 loss.  The gradients compute Z again, a piece of the
+ * classes at a time (at most 8192 of them, or 256 MB of dZ where that is more; several pieces have
+ * about as many each); a piece's dZ is held in the layer's type, one rounding
  * (16-bit types: times a factor that puts the largest finite |g| T at 2^15, so that
  * neither large nor small g leave fp16's range), dX is added up over the pieces in fp32,
  * and each result is rounded once: a 16-bit dX or dF is off by up to about 1.4 roundings

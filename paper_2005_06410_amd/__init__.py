@@ -846,7 +846,8 @@ def linear_cross_entropy_backward(F, X, labels, lse, dloss, bias=None, ignore_in
         dZ[m, n] = dloss[n] (exp(Z[m, n] - lse[n]) - [m == labels[n]]),
         dX = F^T dZ,    dF = dZ X^T,    dbias = dZ 1.
 
-    Z is computed again, a piece of 8192 classes or more at a time; a piece's dZ is
+    Z is computed again, a piece of the classes at a time (at most 8192, or 256 MB of dZ
+    where that is more); a piece's dZ is
     rounded to the layer's type once (16-bit types: times a factor, so that its range does
     not matter), dX is summed over the pieces in float32.  Ignored tokens, and tokens with dloss = 0, add nothing whatever
     their X holds.  dX is stored like X, dF in F's order; ``needs`` leaves out what is
@@ -1035,6 +1036,8 @@ def group_norm_backward(I, dO, groups: int, mean, rstd, weight=None, bias=None, 
     """(dI, dweight, dbias) of ``group_norm`` from dO = dL/dO and the mean and rstd that it
     returned (``convgemm_group_norm_backward``).  dI is stored like I with no gaps; without
     a weight or bias the derivative is still that by a weight of ones or a bias of zeros.
+    relu's slope goes by Z as computed from the float32 mean and rstd, within whose
+    roundings of 0 it may be either.
     ``needs`` leaves out what is not wanted (None is returned in its place)."""
     sizes, act, dtype, dev, dist, (wp, bp) = _norm_args(I, groups, weight, bias, activation)
     distd = _map_strides(dO, I.shape, "dO", dtype, dev)[1:]

@@ -10,8 +10,8 @@
 //   tokens of 1000 channels bf16, GELU: 12 us, gradients 14 (through LDS: 23 and 34).
 // * resident: a unit of whole groups in a workgroup's registers, one read and one write.  27 x
 //   27 x 256 x 80 fp32, 32 groups: 26 us (4.6 TB/s), gradients 40 (4.5 TB/s).
-// * split, for larger maps: two reads.  256 x 256 x 128 x 16 bf16: 49 us for the statistics
-//   (5.5 TB/s), 92 for the result (5.9), 101 and 137 for the gradients (5.3 and 5.9).  Rounds of
+// * split, for larger maps: two reads.  256 x 256 x 128 x 16 bf16: 50 us for the statistics
+//   (5.4 TB/s), 92 for the result (5.9), 102 and 138 for the gradients (5.2 and 5.8).  Rounds of
 //   images that the last-level cache could hold from the first pass to the second were no
 //   faster (162 us instead of 146 forward): the second read is not what bounds it, and each round adds three launches.
 #pragma once
