@@ -139,7 +139,9 @@ struct Count {
   float n, inverse;
   __device__ explicit Count(float v) : n(v), inverse(1.0f / v) {}
   __device__ float quotient(float sum, float* lost = nullptr) const {
-    const float first = sum * inverse, q = fmaf(fmaf(-first, n, sum), inverse, first);
+    const float first = sum * inverse;
+    if (!(fabsf(first) < INFINITY)) return first;        // nothing is lost of it, and inf - inf is not inf
+    const float q = fmaf(fmaf(-first, n, sum), inverse, first);
     if (lost) *lost = fmaf(-q, n, sum) * inverse;
     return q;
   }
@@ -149,7 +151,7 @@ struct Count {
 // quotient and the sum with what their roundings lose, the hardware's root and one step of
 // Newton's.
 __device__ inline float rstd_of(float sum, const Count& n, float eps) {
-  float lost;
+  float lost = 0.0f;
   const float q = n.quotient(sum, &lost), v = q + eps, e = v - q;
   lost += (q - (v - e)) + (eps - e);
   // no sum of normal size (0 and NaN among them) has a finite root to go on from

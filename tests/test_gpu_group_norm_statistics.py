@@ -144,3 +144,19 @@ def test_gradients_of_scaled_inputs(shape, groups, dtype):
         # what is near bf16's or fp32's smallest values is rounded there
         assert torch.equal(torch.where(want[0].abs() < 2.0 ** -60, 0, got[0]), torch.where(want[0].abs() < 2.0 ** -60, 0, want[0]) * 2.0 ** k)
         assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape,groups", ONE_READ)
+def test_squares_and_sums_beyond_the_range(shape, groups, dtype):
+    """Squares that leave fp32's range make rstd 0 and O the bias; a sum that does makes the mean
+    infinite."""
+    c, s, b = shape
+    n = c // groups * s
+    sign = (torch.arange(n, device="cuda") % 2 * 2 - 1.0) * (torch.arange(n, device="cuda") < n // 2 * 2)
+    x = stored((sign * 1e20)[None, :, None].expand(groups, n, b).reshape(shape), dtype)
+    bias = torch.randn(c, generator=gen(c), device="cuda").to(dtype)
+    o, mean, rstd = lt().group_norm(x, groups, bias=bias)
+    assert (mean == 0).all() and (rstd == 0).all() and torch.equal(o, bias[:, None, None].expand(shape))
+    _, mean, _ = lt().group_norm(stored(torch.full(shape, 3e38, device="cuda"), dtype), groups)
+    assert (mean == torch.inf).all()
