@@ -971,7 +971,7 @@ def _span(v, b: int, s: int, c: int, ld: int, ldb: int):
 
 def _maps_meet(c: int, s: int, b: int, x: int, ldx: int, ldbx: int, o: int, ldo: int, ldbo: int) -> bool:
     """Whether two maps of c s b values (at the addresses x and o, in values) share one.
-    Maps at different distances of which both have gaps are taken to where their spans
+    Maps at different distances, both with gaps, are taken to share one where their spans
     meet."""
     if c * s * b == 0:
         return False
